@@ -174,7 +174,7 @@ def _own(s):
             s.opt = binding.BlockNorm(kind=(binding.NORM_RMS, binding.NORM_LAYER)[NORMS.index(c["kind"])], eps=EPS, residual_scale=c["alpha"],
                                       branch_scale=c["beta"], dropout_p=c["p"], gate_rows=c["gate_rows"])
             if c["direction"] == "backward":
-                nbytes = binding.block_norm_workspace_bytes(c["tokens"], c["width"], c["gate_rows"])
+                nbytes = binding.block_norm_workspace_bytes(c["tokens"], c["width"])
         s.ws = torch.empty(max(int(nbytes), 256), dtype=torch.uint8, device="cuda")
     lrd = s.lib
     if c["op"] == "dropout":
