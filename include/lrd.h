@@ -295,7 +295,7 @@ lrd_status lrd_linear_wgrad_batched(const void* dY, int64_t dy_stride, const voi
  * act = LRD_ACT_NONE makes them identical to the plain calls (Y_act / Z_in ignored).  Results are
  * bit-identical to the plain call followed by lrd_gelu_fwd / lrd_gelu_bwd.
  */
-enum { LRD_ACT_NONE = 0, LRD_ACT_GELU = 1 };
+enum { LRD_ACT_NONE = 0, LRD_ACT_GELU = 1, LRD_ACT_SILU = 2 };      /* SILU: the gated calls only */
 lrd_status lrd_linear_fwd_act(const void* X, const void* V, const void* U, const float* bias,
                               void* Y, void* Y_act, void* H_save, int32_t act, int64_t T,
                               int64_t in, int64_t out, int64_t r, lrd_dtype dt, void* ws,
@@ -305,6 +305,38 @@ lrd_status lrd_linear_bwd_act(const void* dY, const void* X, const void* H, cons
                               uint32_t freeze_mask, const void* Z_in, int32_t act, int64_t T,
                               int64_t in, int64_t out, int64_t r, lrd_dtype dt, void* ws,
                               size_t ws_bytes, void* hip_stream);
+
+/*
+ * Gated pair: two decomposed layers of one shape on the same input, joined as a gated feed-forward block
+ * begins (not part of the paper's method):
+ *     H = X.V_cat^T,  Zg = Hg.Ug^T (+ bg),  Zu = Hu.Uu^T (+ bu),  A = act(Zg) * Zu  (elementwise).
+ * The layouts are those of a group of two: V_cat [2*r x in] (the gate's factor in rows 0 .. r - 1, the other's
+ * behind it), U [2][out x r], bias [2][out] fp32 or NULL, H_save / H [T x 2*r] = [Hg | Hu], dV_cat [2*r x in],
+ * dU [2][out x r], dbias [2][out] fp32 or NULL.  A and dA are [T x out].  act: LRD_ACT_NONE, _GELU (erf form)
+ * or _SILU (z / (1 + exp(-z))).  Zg and Zu are not stored, forward or backward: the backward computes them
+ * again from H.  H, dZ and dH are rounded to dtype dt, and what follows starts from the rounded values; Zg, Zu
+ * and the activation stay in fp32 until A, or dZ, is rounded.
+ *   lrd_linear_gated_fwd: H_save may be NULL.
+ *   lrd_linear_gated_bwd: dZg = dA * Zu * act'(Zg), dZu = dA * act(Zg), and from dZ what lrd_linear_group_bwd makes of
+ *     the outputs' gradient: dX [T x in] (the sum of both layers'; NULL: not wanted), dV_cat unless LRD_FREEZE_L0, dU unless
+ *     LRD_FREEZE_L1, dbias.  H NULL: computed again from X.  X is required if V_cat is trainable or H is NULL.
+ *   lrd_linear_gated_bwd_data: the data gradient alone, for a backward in two parts.  dZ [2][T x out] and dH_save
+ *     [T x 2*r], caller's, required, receive what lrd_linear_wgrad_batched needs (dZ in the place of dY).  dX may be NULL.
+ * Workspace for all three from lrd_linear_gated_workspace_bytes.  No output may overlap an input.
+ */
+size_t lrd_linear_gated_workspace_bytes(int64_t T, int64_t in, int64_t out, int64_t r, lrd_dtype dt,
+                                        uint32_t freeze_mask);
+lrd_status lrd_linear_gated_fwd(const void* X, const void* V_cat, const void* U, const float* bias, void* A,
+                                void* H_save, int32_t act, int64_t T, int64_t in, int64_t out, int64_t r,
+                                lrd_dtype dt, void* ws, size_t ws_bytes, void* hip_stream);
+lrd_status lrd_linear_gated_bwd(const void* dA, const void* X, const void* H, const void* V_cat, const void* U,
+                                const float* bias, void* dX, float* dV_cat, float* dU, float* dbias,
+                                uint32_t freeze_mask, int32_t act, int64_t T, int64_t in, int64_t out, int64_t r,
+                                lrd_dtype dt, void* ws, size_t ws_bytes, void* hip_stream);
+lrd_status lrd_linear_gated_bwd_data(const void* dA, const void* H, const void* V_cat, const void* U,
+                                     const float* bias, void* dX, void* dZ, void* dH_save, int32_t act, int64_t T,
+                                     int64_t in, int64_t out, int64_t r, lrd_dtype dt, void* ws, size_t ws_bytes,
+                                     void* hip_stream);
 
 /*
  * The undecomposed layer Y = X.W^T (+ bias), dX = dY.W, dW = dY^T.X: the "original layer" whose
@@ -432,6 +464,65 @@ lrd_status lrd_tucker2_factors(const float* W, int64_t S, int64_t C, int32_t k, 
 lrd_status lrd_gelu_fwd(const void* Z, void* A, int64_t n, lrd_dtype dt, void* hip_stream);
 lrd_status lrd_gelu_bwd(const void* dA, const void* Z, void* dZ, int64_t n, lrd_dtype dt,
                         void* hip_stream);
+
+/*
+ * What stands between two blocks of a network: the norm behind a block, its gate, dropout, the residual sum and the
+ * norm before the next block, in one pass over the rows.  For each token of the block's result F and the stream X
+ * (both [T x d], dtype dt):
+ *     z = norm(F) * w_post + b_post   (w_post NULL: z = F),
+ *     Y = residual_scale * X + branch_scale * drop(gate * z),
+ *     N = norm(Y) * w_pre + b_pre     (N NULL: no norm before the next block).
+ * norm: LRD_NORM_RMS x / sqrt(mean(x^2) + eps), or LRD_NORM_LAYER (x - mean) / sqrt(mean((x - mean)^2) + eps).  drop: as
+ * lrd_dropout with dropout_p on the dense [T x d] array (the same mask).  w_*, b_* [d] fp32; b_* may be NULL.
+ * gate [groups x d] fp32 or NULL: token t has row t / gate_rows (a learned scale: one row, gate_rows 0 or >= T; a gate for each
+ * sequence: its tokens; groups = ceil(T / gate_rows)).
+ * F NULL (before the first block): N is the norm of X; Y is not written and w_post, b_post, gate, dropout_p and the scales are
+ * ignored.  N goes by the unrounded Y.  Y and N may each be F or X (not each other): a row is read before it is written.
+ * Everything between is fp32.  rng as for lrd_dropout; required if dropout_p rounds to more than 0.
+ * 1 <= d <= LRD_BLOCK_NORM_MOST_WIDTH (LRD_ERR_UNSUPPORTED beyond); eps >= 0.
+ */
+enum { LRD_NORM_RMS = 0, LRD_NORM_LAYER = 1 };
+#define LRD_BLOCK_NORM_MOST_WIDTH 16384
+typedef struct {
+    int32_t kind;              /* LRD_NORM_*, of both norms */
+    float eps;
+    float residual_scale, branch_scale;
+    double dropout_p;
+    int64_t gate_rows;
+} lrd_block_norm;
+lrd_status lrd_block_norm_fwd(const void* F, const void* X, const float* w_post, const float* b_post, const float* gate,
+                              const float* w_pre, const float* b_pre, const uint64_t* rng, void* Y, void* N,
+                              const lrd_block_norm* opt, int64_t T, int64_t d, lrd_dtype dt, void* hip_stream);
+
+/*
+ * Backward: from dY, the gradient of the stream that comes back past the next block, and dN, that of its input (either may be
+ * NULL), F and Y as the forward pass had and wrote them (statistics are computed again; N's gradient goes by the stored Y).
+ *   dX, dF [T x d] (nullable): gradients of X and F.  dw_post, db_post, dw_pre, db_pre [d], dgate [groups x d] fp32 (nullable):
+ *   sums over the tokens in a fixed order, overwritten.  dX and dF may each be dY, dN, F or Y (not each other).
+ *   Y is required with dN (F NULL in the forward: Y is X there).  F is required for dgate, and where w_post is given for dF too.
+ *   w_pre is required with dN; b_post only for dgate (z contains it).  Without w_post there is no dw_post, db_post; without
+ *   dN no dw_pre, db_pre; without gate no dgate: asking for one is LRD_ERR_INVALID_ARG.
+ *   A stream without a block (F NULL in the forward) has only dX, dw_pre and db_pre, with residual_scale 1.
+ * Workspace from lrd_block_norm_workspace_bytes (only where a sum over tokens is wanted; it serves every gate_rows).
+ */
+size_t lrd_block_norm_workspace_bytes(int64_t T, int64_t d);
+lrd_status lrd_block_norm_bwd(const void* dY, const void* dN, const void* F, const void* Y, const float* w_post,
+                              const float* b_post, const float* gate, const float* w_pre, const uint64_t* rng, void* dX,
+                              void* dF, float* dw_post, float* db_post, float* dgate, float* dw_pre, float* db_pre,
+                              const lrd_block_norm* opt, int64_t T, int64_t d, lrd_dtype dt, void* ws, size_t ws_bytes,
+                              void* hip_stream);
+
+/*
+ * Dropout of n elements of the activation dtype: Y = X * scale where an element is kept, else 0 (whatever X holds there); Y may be
+ * X.  The mask is a function of rng and the element's index i alone and is stored nowhere; the gradient is the same call on dY.
+ *   rng   device, two uint64, 16-byte aligned: a seed and the number of this call.  Calls with different numbers (or seeds) have
+ *         unrelated masks; a captured graph reads them at each replay, so a program counts on by adding to rng[1] between replays.
+ *   Element i has 16 bits, half i % 2 of word i / 2 % 4 of Philox4x32-10 (Salmon, Moraes, Dror, Shaw 2011) with counter
+ *   (low, high half of i / 8, low, high half of rng[1]) and key (low, high half of rng[0]).  It is dropped where they are below
+ *   D = p * 65536 rounded to nearest, ties to even; scale = 65536 / (65536 - D).  0 <= p <= 1; D = 0 copies (rng may be NULL),
+ *   D = 65536 writes zeros.
+ */
+lrd_status lrd_dropout(const void* X, void* Y, int64_t n, double p, const uint64_t* rng, lrd_dtype dt, void* hip_stream);
 
 #ifdef __cplusplus
 }

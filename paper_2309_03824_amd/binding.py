@@ -22,7 +22,8 @@ FREEZE_L0, FREEZE_L1, FREEZE_L2 = 1, 2, 4
 FUSION_AUTO, FUSION_ALWAYS, FUSION_NEVER = 0, 1, 2
 ROLE_NONE, ROLE_FWD_DOWN, ROLE_FWD_UP, ROLE_DGRAD_UP, ROLE_DGRAD_DOWN, ROLE_WGRAD_U, ROLE_WGRAD_V, ROLE_SUMS = range(8)
 ROUND_NEAREST, ROUND_DOWN, ROUND_UP = 0, 1, 2
-ACT_NONE, ACT_GELU = 0, 1
+ACT_NONE, ACT_GELU, ACT_SILU = 0, 1, 2
+NORM_RMS, NORM_LAYER = 0, 1
 
 EXPORTS = (
     "lrd_status_string", "lrd_quantize_rank", "lrd_freeze_mask", "lrd_tucker_rank", "lrd_svd_rank", "lrd_select_rank",
@@ -36,6 +37,8 @@ EXPORTS = (
     "lrd_tucker_conv_workspace_bytes", "lrd_tucker_conv_fwd", "lrd_tucker_conv_bwd",
     "lrd_dense_conv_workspace_bytes", "lrd_dense_conv_fwd", "lrd_dense_conv_bwd",
     "lrd_gelu_fwd", "lrd_gelu_bwd",
+    "lrd_linear_gated_workspace_bytes", "lrd_linear_gated_fwd", "lrd_linear_gated_bwd", "lrd_linear_gated_bwd_data",
+    "lrd_block_norm_fwd", "lrd_block_norm_workspace_bytes", "lrd_block_norm_bwd", "lrd_dropout",
 )
 # measurement aids (include/lrd_measure.h): not part of the layer ABI
 MEASURE_EXPORTS = ("lrd_set_fusion", "lrd_profile_log_start", "lrd_profile_log_stop", "lrd_measure_mfma_loop", "lrd_measure_lds_read", "lrd_measure_stream")
@@ -50,6 +53,15 @@ class LrdError(RuntimeError):
 
 class Sgd(Structure):
     _fields_ = [("lr", ctypes.c_float), ("momentum", ctypes.c_float), ("weight_decay", ctypes.c_float)]
+
+
+class BlockNorm(Structure):
+    """lrd_block_norm: what block_norm_fwd / _bwd compute between two blocks (gate_rows: tokens that share a row of the gate, 0 for all)."""
+    _fields_ = [("kind", c_int32), ("eps", ctypes.c_float), ("residual_scale", ctypes.c_float), ("branch_scale", ctypes.c_float),
+                ("dropout_p", c_double), ("gate_rows", c_int64)]
+
+    def __init__(self, kind=NORM_RMS, eps=1e-5, residual_scale=1.0, branch_scale=1.0, dropout_p=0.0, gate_rows=0):
+        super().__init__(kind, eps, residual_scale, branch_scale, dropout_p, gate_rows)
 
 
 class ProfileRecord(Structure):
@@ -163,6 +175,22 @@ def _load() -> ctypes.CDLL:
     lib.lrd_set_fusion.argtypes = [c_int32]
     lib.lrd_gelu_bwd.restype = ctypes.c_int
     lib.lrd_gelu_bwd.argtypes = [P, P, P, I64, ctypes.c_int, P]
+    lib.lrd_linear_gated_workspace_bytes.restype = SZ
+    lib.lrd_linear_gated_workspace_bytes.argtypes = [I64] * 4 + [ctypes.c_int, U32]
+    lib.lrd_linear_gated_fwd.restype = ctypes.c_int
+    lib.lrd_linear_gated_fwd.argtypes = [P] * 6 + [c_int32] + [I64] * 4 + [ctypes.c_int, P, SZ, P]
+    lib.lrd_linear_gated_bwd.restype = ctypes.c_int
+    lib.lrd_linear_gated_bwd.argtypes = [P] * 10 + [U32, c_int32] + [I64] * 4 + [ctypes.c_int, P, SZ, P]
+    lib.lrd_linear_gated_bwd_data.restype = ctypes.c_int
+    lib.lrd_linear_gated_bwd_data.argtypes = [P] * 8 + [c_int32] + [I64] * 4 + [ctypes.c_int, P, SZ, P]
+    lib.lrd_block_norm_fwd.restype = ctypes.c_int
+    lib.lrd_block_norm_fwd.argtypes = [P] * 10 + [POINTER(BlockNorm), I64, I64, ctypes.c_int, P]
+    lib.lrd_block_norm_workspace_bytes.restype = SZ
+    lib.lrd_block_norm_workspace_bytes.argtypes = [I64, I64]
+    lib.lrd_block_norm_bwd.restype = ctypes.c_int
+    lib.lrd_block_norm_bwd.argtypes = [P] * 16 + [POINTER(BlockNorm), I64, I64, ctypes.c_int, P, SZ, P]
+    lib.lrd_dropout.restype = ctypes.c_int
+    lib.lrd_dropout.argtypes = [P, P, I64, c_double, P, ctypes.c_int, P]
     lib.lrd_measure_mfma_loop.restype = ctypes.c_int
     lib.lrd_measure_mfma_loop.argtypes = [P, c_int32, c_int32, POINTER(c_double), P]
     lib.lrd_measure_lds_read.restype = ctypes.c_int
@@ -390,6 +418,34 @@ class ProfileLog:
         return out
 
 
+def _same(like, shape, *tensors):
+    """Pointers of tensors of `like`'s type and device and of `shape` (None stays None)."""
+    for t in tensors:
+        if t is not None and (t.dtype != like.dtype or t.shape != shape or t.device != like.device):
+            raise ValueError(f"{like.dtype} tensor of shape {tuple(shape)} on {like.device} expected, not {t.dtype} {tuple(t.shape)} on {t.device}")
+    return [_ptr(t) for t in tensors]
+
+
+def _f32s(like, *pairs):
+    """Pointers of fp32 tensors on `like`'s device: (tensor or None, shape) each."""
+    for t, shape in pairs:
+        if t is not None and (t.dtype != torch.float32 or t.shape != shape or t.device != like.device):
+            raise ValueError(f"torch.float32 tensor of shape {tuple(shape)} on {like.device} expected, not {t.dtype} {tuple(t.shape)} on {t.device}")
+    return [_ptr(t) for t, _ in pairs]
+
+
+def _here(t):
+    """The current device, whose stream a call takes, has to be the tensors'."""
+    if t.is_cuda and t.device.index != torch._C._cuda_getDevice():
+        raise ValueError(f"tensors on {t.device}, but the current device is cuda:{torch._C._cuda_getDevice()}")
+
+
+def _rng(like, rng):
+    if rng is not None and (rng.dtype not in (torch.int64, torch.uint64) or rng.numel() != 2 or rng.device != like.device):
+        raise ValueError("rng is two 64-bit integers (seed, call) on the tensors' device")
+    return _ptr(rng)
+
+
 # ------------------------------------------------------------------------------- linear pair
 def linear_workspace_bytes(T, n_in, n_out, r, dtype, freeze_mask=0) -> int:
     return int(_lib.lrd_linear_workspace_bytes(T, n_in, n_out, r, dtype, freeze_mask))
@@ -527,6 +583,60 @@ def linear_wgrad_batched(dY, H, dH, X, dV, dU, freeze_mask, ws=None, stream=None
                                          freeze_mask, L, T, n_in, n_out, r, dt, wp, wb, _stream(stream)), "lrd_linear_wgrad_batched")
 
 
+def linear_gated_workspace_bytes(T, n_in, n_out, r, dtype, freeze_mask=0) -> int:
+    return int(_lib.lrd_linear_gated_workspace_bytes(T, n_in, n_out, r, dtype, freeze_mask))
+
+
+def linear_gated_fwd(X, V_cat, U, bias, A, H_save, act, ws=None, stream=None):
+    """A [T, out] = act(Zg) * Zu of a gated pair; U [2, out, r] (the gate's first), V_cat [2r, in], bias [2, out] or None, H_save [T, 2r] or None."""
+    T, n_in = X.shape
+    _, n_out, r = U.shape
+    _here(X)
+    x, = _same(X, (T, n_in), X)
+    v, = _same(X, (2 * r, n_in), V_cat)
+    u, = _same(X, (2, n_out, r), U)
+    a, = _same(X, (T, n_out), A)
+    h, = _same(X, (T, 2 * r), H_save)
+    b, = _f32s(X, (bias, (2, n_out)))
+    wp, wb = _ws(ws)
+    _check(_lib.lrd_linear_gated_fwd(x, v, u, b, a, h, act, T, n_in, n_out, r, _dt(X), wp, wb, _stream(stream)), "lrd_linear_gated_fwd")
+
+
+def linear_gated_bwd(dA, X, H, V_cat, U, bias, dX, dV_cat, dU, dbias, freeze_mask, act, ws=None, stream=None):
+    """All gradients of a gated pair from dA [T, out]; H as saved by the forward, or None (computed again from X)."""
+    T, n_out = dA.shape
+    _, _, r = U.shape
+    n_in = V_cat.shape[1]
+    _here(dA)
+    d, = _same(dA, (T, n_out), dA)
+    x, dx = _same(dA, (T, n_in), X, dX)
+    h, = _same(dA, (T, 2 * r), H)
+    v, = _same(dA, (2 * r, n_in), V_cat)
+    u, = _same(dA, (2, n_out, r), U)
+    b, dv, du, db = _f32s(dA, (bias, (2, n_out)), (dV_cat, (2 * r, n_in)), (dU, (2, n_out, r)), (dbias, (2, n_out)))
+    wp, wb = _ws(ws)
+    _check(_lib.lrd_linear_gated_bwd(d, x, h, v, u, b, dx, dv, du, db, freeze_mask, act, T, n_in, n_out, r, _dt(dA), wp, wb, _stream(stream)),
+           "lrd_linear_gated_bwd")
+
+
+def linear_gated_bwd_data(dA, H, V_cat, U, bias, dX, dZ, dH_save, act, ws=None, stream=None):
+    """Data gradient only; dZ [2, T, out] and dH_save [T, 2r] receive what linear_wgrad_batched takes (dZ in the place of dY)."""
+    T, n_out = dA.shape
+    _, _, r = U.shape
+    n_in = V_cat.shape[1]
+    _here(dA)
+    d, = _same(dA, (T, n_out), dA)
+    h, dh = _same(dA, (T, 2 * r), H, dH_save)
+    v, = _same(dA, (2 * r, n_in), V_cat)
+    u, = _same(dA, (2, n_out, r), U)
+    dx, = _same(dA, (T, n_in), dX)
+    dz, = _same(dA, (2, T, n_out), dZ)
+    b, = _f32s(dA, (bias, (2, n_out)))
+    wp, wb = _ws(ws)
+    _check(_lib.lrd_linear_gated_bwd_data(d, h, v, u, b, dx, dz, dh, act, T, n_in, n_out, r, _dt(dA), wp, wb, _stream(stream)),
+           "lrd_linear_gated_bwd_data")
+
+
 def linear_fwd_act(X, V, U, bias, Y, Y_act, H_save, act, ws=None, stream=None):
     T, n_in = X.shape
     r, n_out = V.shape[0], U.shape[0]
@@ -611,3 +721,43 @@ def gelu_fwd(Z, A, stream=None):
 
 def gelu_bwd(dA, Z, dZ, stream=None):
     _check(_lib.lrd_gelu_bwd(_ptr(dA), _ptr(Z), _ptr(dZ), Z.numel(), _dt(Z), _stream(stream)), "lrd_gelu_bwd")
+
+
+def dropout(X, Y, p, rng, stream=None):
+    """Y = X / (1 - p) where the generator keeps an element, else 0; rng: int64 tensor (seed, number of the call).  The gradient is the
+    same call on dY."""
+    _here(X)
+    x, y = _same(X, X.shape, X, Y)
+    _check(_lib.lrd_dropout(x, y, X.numel(), p, _rng(X, rng), _dt(X), _stream(stream)), "lrd_dropout")
+
+
+def _gate_rows(opt: "BlockNorm", T, d):
+    return (-(-T // opt.gate_rows) if opt.gate_rows > 0 else 1, d)
+
+
+def block_norm_fwd(F, X, w_post, b_post, gate, w_pre, b_pre, rng, Y, N, opt: "BlockNorm", stream=None):
+    """Y = residual_scale X + branch_scale drop(gate * norm_post(F)), N = norm_pre(Y); see lrd_block_norm_fwd for what may be None."""
+    T, d = X.shape
+    _here(X)
+    f, x, y, n = _same(X, (T, d), F, X, Y, N)
+    wo, bo, g, wi, bi = _f32s(X, (w_post, (d,)), (b_post, (d,)), (gate, _gate_rows(opt, T, d)), (w_pre, (d,)), (b_pre, (d,)))
+    _check(_lib.lrd_block_norm_fwd(f, x, wo, bo, g, wi, bi, _rng(X, rng), y, n, ctypes.byref(opt), T, d, _dt(X), _stream(stream)), "lrd_block_norm_fwd")
+
+
+def block_norm_workspace_bytes(T, d) -> int:
+    return int(_lib.lrd_block_norm_workspace_bytes(T, d))
+
+
+def block_norm_bwd(dY, dN, F, Y, w_post, b_post, gate, w_pre, rng, dX, dF, dw_post, db_post, dgate, dw_pre, db_pre, opt: "BlockNorm", ws=None,
+                   stream=None):
+    """Gradients of block_norm_fwd from dY and dN (either may be None); see lrd_block_norm_bwd for what may be None."""
+    like = dY if dY is not None else dN
+    T, d = like.shape
+    _here(like)
+    dy, dn, f, y, dx, df = _same(like, (T, d), dY, dN, F, Y, dX, dF)
+    gs = _gate_rows(opt, T, d)
+    wo, bo, g, wi = _f32s(like, (w_post, (d,)), (b_post, (d,)), (gate, gs), (w_pre, (d,)))
+    dwo, dbo, dg, dwi, dbi = _f32s(like, (dw_post, (d,)), (db_post, (d,)), (dgate, gs), (dw_pre, (d,)), (db_pre, (d,)))
+    wp, wb = _ws(ws)
+    _check(_lib.lrd_block_norm_bwd(dy, dn, f, y, wo, bo, g, wi, _rng(like, rng), dx, df, dwo, dbo, dg, dwi, dbi, ctypes.byref(opt), T, d, _dt(like), wp,
+                                   wb, _stream(stream)), "lrd_block_norm_bwd")

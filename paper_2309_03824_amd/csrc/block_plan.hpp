@@ -1,0 +1,46 @@
+// How the rows of a block norm's backward pass are dealt to workgroups (see block_norm.inc).
+#pragma once
+#include <algorithm>
+#include <cstdint>
+
+namespace lrd {
+
+enum { BN_W_PRE, BN_B_PRE, BN_W_POST, BN_B_POST, BN_SUMS };     // partial rows of a workgroup
+
+// Units of rows, none across two rows of the gate: `by_slot`, a group of gate_rows rows each, for one of a workgroup's slots;
+// else `parts` of part_rows rows in each group (the last ones of the last group may be empty), for a workgroup.
+struct BlockNormPlan {
+    int64_t gate_rows, units, parts, part_rows, workgroups;
+    bool by_slot;
+};
+
+inline int64_t block_norm_slots(int64_t d) { return d <= 1024 ? 8 : 1; }      // rows that a workgroup works on at once
+
+inline BlockNormPlan block_norm_plan(int64_t T, int64_t d, int64_t gate_rows)
+{
+    auto up = [](int64_t a, int64_t b) { return (a + b - 1) / b; };
+    constexpr int64_t MOST = 512;                   // workgroups: two to a compute unit
+    const int64_t slots = block_norm_slots(d);
+    BlockNormPlan p;
+    p.gate_rows = gate_rows > 0 && gate_rows < T ? gate_rows : T;
+    const int64_t groups = up(T, p.gate_rows);
+    p.by_slot = groups > 1 && p.gate_rows <= 16;
+    if (p.by_slot) {
+        p.units = groups; p.parts = 1; p.part_rows = p.gate_rows;
+        p.workgroups = std::min(MOST, up(groups, slots));
+        return p;
+    }
+    // parts of a group so that there is a unit for each workgroup, and no smaller than a round of its slots
+    const int64_t wanted = up(std::min(MOST, up(T, slots)), groups);
+    p.part_rows = std::max(slots, up(p.gate_rows, wanted));
+    p.parts = up(p.gate_rows, p.part_rows);
+    p.units = groups * p.parts;
+    p.workgroups = std::min(MOST, p.units);
+    return p;
+}
+
+// Most workgroups and gate units over every gate for T tokens or fewer: partial rows that a workspace has room for.
+inline int64_t block_norm_most_workgroups(int64_t T) { return std::min<int64_t>(512, 2 * T); }
+inline int64_t block_norm_most_units(int64_t T) { return std::min<int64_t>(1024, 2 * T); }
+
+}  // namespace lrd

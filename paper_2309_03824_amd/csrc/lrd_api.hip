@@ -2,8 +2,11 @@
 // pass out of matrix products (see lrd.h for the contract of every call).
 #include <algorithm>
 #include <atomic>
+#include <cmath>
 #include <mutex>
 
+#include "block_norm.hpp"
+#include "gated.hpp"
 #include "lrd.h"
 #include "lrd_internal.hpp"
 #include "lrd_measure.h"
@@ -856,6 +859,178 @@ lrd_status lrd_linear_wgrad_batched(const void* dY, int64_t dy_stride, const voi
     return LRD_OK;
 }
 
+// ------------------------------------------------------------------------------------ gated pair
+// A group of two whose outputs are joined where they are computed; the backward makes the gradients of both outputs first and
+// is then the group's.
+namespace {
+inline bool act_ok(int32_t act) { return act == LRD_ACT_NONE || act == LRD_ACT_GELU || act == LRD_ACT_SILU; }
+
+// What lrd_linear_group_bwd takes of its workspace for two layers with H given.
+size_t gated_group_bytes(int64_t T, int64_t in, int64_t out, int64_t r, lrd_dtype dt, bool need_dH, Tokens tokens)
+{
+    return (need_dH ? round256((size_t)T * 2 * r * esize(dt)) : 0) + round256(group_partial_region(T, in, out, r, 2, dt, true, tokens));
+}
+// Padded copies of U, V_cat and H, and, for a whole backward, of dU and dV_cat.
+size_t gated_pad_bytes(int64_t T, int64_t in, int64_t out, int64_t r8, bool grads)
+{
+    return round256((size_t)2 * out * r8 * 2) + round256((size_t)2 * r8 * in * 2) + round256((size_t)T * 2 * r8 * 2) +
+           (grads ? round256((size_t)2 * out * r8 * 4) + round256((size_t)2 * r8 * in * 4) : 0);
+}
+
+GatedOp gated_op(const void* H, const void* U, const float* bias, int64_t T, int64_t out, int64_t r, int32_t act, lrd_dtype dt)
+{
+    GatedOp op{};
+    op.H = H; op.U = U; op.bias = bias;
+    op.T = T; op.out = out; op.r = r; op.act = act; op.bf16 = dt == LRD_BF16;
+    return op;
+}
+// Zero-padded copies of a group of two's factors and intermediate at rank r8 (any of them null).
+hipError_t pad_gated(const void* U, void* Up, const void* V, void* Vp, const void* H, void* Hp, int64_t T, int64_t in, int64_t out, int64_t r,
+                     int64_t r8, hipStream_t st)
+{
+    CopyJob jobs[4];
+    int n = 0;
+    if (U) jobs[n++] = {U, 2 * out, r, Up, 2 * out, r8, 2};
+    if (V) {
+        jobs[n++] = {V, r, in, Vp, r8, in, 2};
+        jobs[n++] = {(const char*)V + r * in * 2, r, in, (char*)Vp + r8 * in * 2, r8, in, 2};
+    }
+    if (H) jobs[n++] = {H, 2 * T, r, Hp, 2 * T, r8, 2};
+    return copy2d(jobs, n, st);
+}
+}  // namespace
+
+size_t lrd_linear_gated_workspace_bytes(int64_t T, int64_t in, int64_t out, int64_t r, lrd_dtype dt, uint32_t freeze_mask)
+{
+    (void)freeze_mask;
+    if (!dtype_ok(dt) || !group_dims_ok(T, in, out, r, 2)) return 0;
+    const bool pads = pads_rank(in, out, r, dt);
+    const int64_t rr = pads ? pad8(r) : r;
+    const size_t H = round256((size_t)T * 2 * rr * esize(dt)), dZ = round256((size_t)2 * T * out * esize(dt));
+    const size_t fwd = H + round256(group_partial_region(T, in, out, rr, 2, dt, false, UP_TO));
+    const size_t bwd = dZ + H + gated_group_bytes(T, in, out, rr, dt, true, UP_TO);
+    const size_t data = H + round256(act_partial_bytes(T, rr, out, dt, UP_TO));
+    return std::max(std::max(fwd, bwd), data) + (pads ? gated_pad_bytes(T, in, out, rr, true) : 0);
+}
+
+lrd_status lrd_linear_gated_fwd(const void* X, const void* V_cat, const void* U, const float* bias, void* A, void* H_save, int32_t act,
+                                int64_t T, int64_t in, int64_t out, int64_t r, lrd_dtype dt, void* ws, size_t ws_bytes, void* hip_stream)
+{
+    if (!dtype_ok(dt) || !act_ok(act) || !group_dims_ok(T, in, out, r, 2) || !X || !V_cat || !U || !A) return LRD_ERR_INVALID_ARG;
+    if (!aligned16(X) || !aligned16(V_cat) || !aligned16(U) || !aligned16(bias) || !aligned16(A) || !aligned16(H_save) || !aligned16(ws))
+        return LRD_ERR_ALIGNMENT;
+    hipStream_t st = (hipStream_t)hip_stream;
+    const bool pads = pads_rank(in, out, r, dt);
+    const int64_t rr = pads ? pad8(r) : r;
+    Carver cv(ws, ws_bytes);
+    void *Up = nullptr, *Vp = nullptr;
+    if (pads) {
+        Up = cv.take((size_t)2 * out * rr * 2);
+        Vp = cv.take((size_t)2 * rr * in * 2);
+    }
+    void* H = H_save && !pads ? H_save : cv.take((size_t)T * 2 * rr * esize(dt));
+    const size_t region_bytes = group_partial_region(T, in, out, rr, 2, dt, false);
+    void* region = region_bytes ? cv.take(region_bytes) : nullptr;
+    if (!cv.ok) return LRD_ERR_WORKSPACE;
+    if (pads) LRD_TRY(pad_gated(U, Up, V_cat, Vp, nullptr, nullptr, T, in, out, r, rr, st));
+    MatOp g1 = nt(X, in, pads ? Vp : V_cat, in, H, 2 * rr, T, 2 * rr, in, dt, false);
+    g1.role = LRD_ROLE_FWD_DOWN;
+    share_splits(g1, region, dt, SPLIT_ACT);
+    LRD_TRY(run_matop(g1, st));
+    GatedOp op = gated_op(H, pads ? Up : U, bias, T, out, rr, act, dt);
+    op.A = A;
+    LRD_TRY(run_gated(op, st));
+    const CopyJob crop = {H, 2 * T, rr, H_save, 2 * T, r, 2};
+    if (pads && H_save) LRD_TRY(copy2d(&crop, 1, st));
+    return LRD_OK;
+}
+
+lrd_status lrd_linear_gated_bwd(const void* dA, const void* X, const void* H, const void* V_cat, const void* U, const float* bias, void* dX,
+                                float* dV_cat, float* dU, float* dbias, uint32_t freeze_mask, int32_t act, int64_t T, int64_t in,
+                                int64_t out, int64_t r, lrd_dtype dt, void* ws, size_t ws_bytes, void* hip_stream)
+{
+    if (!dtype_ok(dt) || !act_ok(act) || !group_dims_ok(T, in, out, r, 2) || !dA || !V_cat || !U) return LRD_ERR_INVALID_ARG;
+    if (freeze_mask & ~uint32_t(LRD_FREEZE_L0 | LRD_FREEZE_L1)) return LRD_ERR_INVALID_ARG;
+    const bool train_v = !(freeze_mask & LRD_FREEZE_L0), train_u = !(freeze_mask & LRD_FREEZE_L1);
+    if ((train_v && (!dV_cat || !X)) || (train_u && !dU) || (!H && !X)) return LRD_ERR_INVALID_ARG;
+    if (!aligned16(dA) || !aligned16(X) || !aligned16(H) || !aligned16(V_cat) || !aligned16(U) || !aligned16(bias) || !aligned16(dX) ||
+        !aligned16(ws) || (train_v && !aligned16(dV_cat)) || (train_u && !aligned16(dU)) || !aligned16(dbias))
+        return LRD_ERR_ALIGNMENT;
+    hipStream_t st = (hipStream_t)hip_stream;
+    const bool need_dH = dX || train_v;
+    if (!need_dH && !train_u && !dbias) return LRD_OK;
+    const bool pads = pads_rank(in, out, r, dt);
+    const int64_t rr = pads ? pad8(r) : r;
+    Carver cv(ws, ws_bytes);
+    void *Up = nullptr, *Vp = nullptr, *dUp = nullptr, *dVp = nullptr;
+    if (pads) {
+        Up = cv.take((size_t)2 * out * rr * 2);
+        Vp = cv.take((size_t)2 * rr * in * 2);
+        dUp = train_u ? cv.take((size_t)2 * out * rr * 4) : nullptr;
+        dVp = train_v ? cv.take((size_t)2 * rr * in * 4) : nullptr;
+    }
+    void* Hw = !H || pads ? cv.take((size_t)T * 2 * rr * esize(dt)) : nullptr;
+    void* dZ = cv.take((size_t)2 * T * out * esize(dt));
+    const size_t rest = gated_group_bytes(T, in, out, rr, dt, need_dH, THESE);
+    char* const rest_at = (char*)ws + cv.used;
+    if (!cv.ok || (rest && !cv.room(rest))) return LRD_ERR_WORKSPACE;
+    if (pads) LRD_TRY(pad_gated(U, Up, V_cat, Vp, H, Hw, T, in, out, r, rr, st));
+    const void *Vc = pads ? Vp : V_cat, *Uc = pads ? Up : U, *Hc = Hw ? Hw : H;
+    if (!H) {
+        MatOp re = nt(X, in, Vc, in, Hw, 2 * rr, T, 2 * rr, in, dt, false);
+        share_splits(re, rest_at, dt, SPLIT_ACT);          // (the group's region holds it: its first product comes later)
+        LRD_TRY(run_matop(re, st));
+    }
+    GatedOp op = gated_op(Hc, Uc, bias, T, out, rr, act, dt);
+    op.dA = dA; op.dZ = dZ;
+    LRD_TRY(run_gated(op, st));
+    const lrd_status rc = lrd_linear_group_bwd(dZ, X, Hc, Vc, Uc, dX, pads ? (float*)dVp : dV_cat, pads ? (float*)dUp : dU, dbias, freeze_mask, T, in,
+                                               out, rr, 2, dt, rest_at, ws_bytes - cv.used, hip_stream);
+    if (rc != LRD_OK || !pads) return rc;
+    CopyJob crops[3];
+    int n = 0;
+    if (train_u) crops[n++] = {dUp, 2 * out, rr, dU, 2 * out, r, 4};
+    if (train_v) {
+        crops[n++] = {dVp, r, in, dV_cat, r, in, 4};
+        crops[n++] = {(const char*)dVp + rr * in * 4, r, in, (char*)dV_cat + r * in * 4, r, in, 4};
+    }
+    LRD_TRY(copy2d(crops, n, st));
+    return LRD_OK;
+}
+
+lrd_status lrd_linear_gated_bwd_data(const void* dA, const void* H, const void* V_cat, const void* U, const float* bias, void* dX, void* dZ,
+                                     void* dH_save, int32_t act, int64_t T, int64_t in, int64_t out, int64_t r, lrd_dtype dt, void* ws,
+                                     size_t ws_bytes, void* hip_stream)
+{
+    if (!dtype_ok(dt) || !act_ok(act) || !group_dims_ok(T, in, out, r, 2) || !dA || !H || !V_cat || !U || !dZ || !dH_save)
+        return LRD_ERR_INVALID_ARG;
+    if (!aligned16(dA) || !aligned16(H) || !aligned16(V_cat) || !aligned16(U) || !aligned16(bias) || !aligned16(dX) || !aligned16(dZ) ||
+        !aligned16(dH_save) || !aligned16(ws))
+        return LRD_ERR_ALIGNMENT;
+    hipStream_t st = (hipStream_t)hip_stream;
+    const bool pads = pads_rank(in, out, r, dt);
+    const int64_t rr = pads ? pad8(r) : r;
+    Carver cv(ws, ws_bytes);
+    void *Up = nullptr, *Vp = nullptr, *Hp = nullptr;
+    if (pads) {
+        Up = cv.take((size_t)2 * out * rr * 2);
+        Vp = cv.take((size_t)2 * rr * in * 2);
+        Hp = cv.take((size_t)T * 2 * rr * 2);          // H, and when dZ is made, dH
+    }
+    const size_t rest = act_partial_bytes(T, rr, out, dt);
+    if (!cv.ok || (rest && !cv.room(rest))) return LRD_ERR_WORKSPACE;
+    if (pads) LRD_TRY(pad_gated(U, Up, V_cat, Vp, H, Hp, T, in, out, r, rr, st));
+    GatedOp op = gated_op(pads ? Hp : H, pads ? Up : U, bias, T, out, rr, act, dt);
+    op.dA = dA; op.dZ = dZ;
+    LRD_TRY(run_gated(op, st));
+    const lrd_status rc = lrd_linear_group_bwd_data(dZ, pads ? Vp : V_cat, pads ? Up : U, dX, pads ? Hp : dH_save, T, in, out, rr, 2, dt,
+                                                    (char*)ws + cv.used, ws_bytes - cv.used, hip_stream);
+    if (rc != LRD_OK || !pads) return rc;
+    const CopyJob crop = {Hp, 2 * T, rr, dH_save, 2 * T, r, 2};
+    LRD_TRY(copy2d(&crop, 1, st));
+    return LRD_OK;
+}
+
 // ------------------------------------------------------------------------------------ dense linear
 size_t lrd_dense_linear_workspace_bytes(int64_t T, int64_t in, int64_t out, lrd_dtype dt)
 {
@@ -1234,6 +1409,100 @@ lrd_status lrd_gelu_bwd(const void* dA, const void* Z, void* dZ, int64_t n, lrd_
     if (!dtype_ok(dt) || n < 0 || !dA || !Z || !dZ) return LRD_ERR_INVALID_ARG;
     if (!aligned16(dA) || !aligned16(Z) || !aligned16(dZ)) return LRD_ERR_ALIGNMENT;
     LRD_TRY(gelu_bwd(dA, Z, dZ, n, dt == LRD_BF16, (hipStream_t)hip_stream));
+    return LRD_OK;
+}
+
+namespace {
+// Dropout's probability as the number of the 65536 values that drop an element; false where p is none.
+bool drop_rng(double p, const uint64_t* state, DropRng* rng)
+{
+    if (!(p >= 0.0 && p <= 1.0)) return false;
+    rng->state = state;
+    rng->below = (uint32_t)std::nearbyint(p * 65536.0);
+    rng->scale = rng->below < 65536u ? (float)(65536.0 / (65536.0 - rng->below)) : 0.f;
+    return !rng->below || state;
+}
+bool block_norm_opt_ok(const lrd_block_norm* o)
+{
+    return o && (o->kind == LRD_NORM_RMS || o->kind == LRD_NORM_LAYER) && o->eps >= 0.f && std::isfinite(o->eps) && std::isfinite(o->residual_scale) &&
+           std::isfinite(o->branch_scale) && o->gate_rows >= 0;
+}
+inline bool block_norm_dims_ok(int64_t T, int64_t d) { return T >= 1 && T < (int64_t(1) << 31) && d >= 1; }
+}  // namespace
+
+lrd_status lrd_dropout(const void* X, void* Y, int64_t n, double p, const uint64_t* rng, lrd_dtype dt, void* hip_stream)
+{
+    DropRng dr;
+    if (!dtype_ok(dt) || n < 0 || !X || !Y || !drop_rng(p, rng, &dr)) return LRD_ERR_INVALID_ARG;
+    if (!aligned16(X) || !aligned16(Y) || !aligned16(rng)) return LRD_ERR_ALIGNMENT;
+    LRD_TRY(dropout(X, Y, n, dt == LRD_BF16, dr, (hipStream_t)hip_stream));
+    return LRD_OK;
+}
+
+lrd_status lrd_block_norm_fwd(const void* F, const void* X, const float* w_post, const float* b_post, const float* gate, const float* w_pre,
+                              const float* b_pre, const uint64_t* rng, void* Y, void* N, const lrd_block_norm* opt, int64_t T, int64_t d,
+                              lrd_dtype dt, void* hip_stream)
+{
+    BlockNormFwd g{};
+    if (!dtype_ok(dt) || !block_norm_dims_ok(T, d) || !block_norm_opt_ok(opt) || !X || (F && !Y) || (N && !w_pre) || (!F && !N)) return LRD_ERR_INVALID_ARG;
+    if (F && ((!w_post && b_post) || !drop_rng(opt->dropout_p, rng, &g.rng))) return LRD_ERR_INVALID_ARG;
+    if (N && N == Y) return LRD_ERR_INVALID_ARG;
+    if (d > BN_MOST_WIDTH) return LRD_ERR_UNSUPPORTED;
+    if (!aligned16(F) || !aligned16(X) || !aligned16(w_post) || !aligned16(b_post) || !aligned16(gate) || !aligned16(w_pre) || !aligned16(b_pre) ||
+        !aligned16(rng) || !aligned16(Y) || !aligned16(N))
+        return LRD_ERR_ALIGNMENT;
+    g.F = F; g.X = X; g.w_post = w_post; g.b_post = b_post; g.gate = gate; g.w_pre = w_pre; g.b_pre = b_pre;
+    g.Y = Y; g.N = N;
+    g.T = T; g.d = (int)d;
+    g.gate_rows = opt->gate_rows ? opt->gate_rows : T;
+    g.layer = opt->kind == LRD_NORM_LAYER; g.eps = opt->eps; g.alpha = opt->residual_scale; g.beta = opt->branch_scale;
+    LRD_TRY((dt == LRD_BF16 ? block_norm_fwd_bf16 : block_norm_fwd_f32)(g, (hipStream_t)hip_stream));
+    return LRD_OK;
+}
+
+size_t lrd_block_norm_workspace_bytes(int64_t T, int64_t d)
+{
+    if (!block_norm_dims_ok(T, d) || d > BN_MOST_WIDTH) return 0;
+    // a partial row for each sum and workgroup, and one of the gate for each unit
+    return round256((size_t)block_norm_most_workgroups(T) * BN_SUMS * d * 4) + round256((size_t)block_norm_most_units(T) * d * 4);
+}
+
+lrd_status lrd_block_norm_bwd(const void* dY, const void* dN, const void* F, const void* Y, const float* w_post, const float* b_post, const float* gate,
+                              const float* w_pre, const uint64_t* rng, void* dX, void* dF, float* dw_post, float* db_post, float* dgate,
+                              float* dw_pre, float* db_pre, const lrd_block_norm* opt, int64_t T, int64_t d, lrd_dtype dt, void* ws, size_t ws_bytes,
+                              void* hip_stream)
+{
+    BlockNormBwd g{};
+    if (!dtype_ok(dt) || !block_norm_dims_ok(T, d) || !block_norm_opt_ok(opt) || (!dY && !dN) || (dN && (!Y || !w_pre))) return LRD_ERR_INVALID_ARG;
+    if ((dw_post || db_post) && !w_post) return LRD_ERR_INVALID_ARG;
+    if ((dw_pre || db_pre) && !dN) return LRD_ERR_INVALID_ARG;
+    if ((dgate && !gate) || (b_post && !w_post)) return LRD_ERR_INVALID_ARG;
+    const bool post = dw_post || db_post || dgate;
+    g.branch = dF || post;
+    if (g.branch && ((!F && (dgate || w_post)) || !drop_rng(opt->dropout_p, rng, &g.rng))) return LRD_ERR_INVALID_ARG;
+    if (dX && dX == dF) return LRD_ERR_INVALID_ARG;
+    if (d > BN_MOST_WIDTH) return LRD_ERR_UNSUPPORTED;
+    if (!aligned16(dY) || !aligned16(dN) || !aligned16(F) || !aligned16(Y) || !aligned16(w_post) || !aligned16(b_post) || !aligned16(gate) ||
+        !aligned16(w_pre) || !aligned16(rng) || !aligned16(dX) || !aligned16(dF) || !aligned16(dw_post) || !aligned16(db_post) ||
+        !aligned16(dgate) || !aligned16(dw_pre) || !aligned16(db_pre) || !aligned16(ws))
+        return LRD_ERR_ALIGNMENT;
+    const BlockNormPlan plan = block_norm_plan(T, d, gate ? opt->gate_rows : 0);
+    Carver cv(ws, ws_bytes);
+    const bool rows = dw_pre || db_pre || dw_post || db_post;
+    if (rows) g.partial = (float*)cv.take((size_t)plan.workgroups * BN_SUMS * d * 4);
+    if (dgate && plan.parts > 1) g.gate_partial = (float*)cv.take((size_t)plan.units * d * 4);
+    if (!cv.ok) return LRD_ERR_WORKSPACE;
+    g.dY = dY; g.dN = dN; g.F = F; g.Y = Y; g.w_post = w_post; g.b_post = b_post; g.gate = gate; g.w_pre = w_pre;
+    g.dX = dX; g.dF = dF; g.dgate = dgate;
+    float* const outs[BN_SUMS] = {dw_pre, db_pre, dw_post, db_post};
+    for (int s = 0; s < BN_SUMS; ++s) g.sums[s] = outs[s] != nullptr;
+    g.T = T; g.d = (int)d;
+    g.gate_rows = plan.gate_rows; g.units = plan.units; g.parts = plan.parts; g.part_rows = plan.part_rows; g.workgroups = plan.workgroups;
+    g.by_slot = plan.by_slot;
+    g.layer = opt->kind == LRD_NORM_LAYER; g.eps = opt->eps; g.alpha = opt->residual_scale; g.beta = opt->branch_scale;
+    hipStream_t st = (hipStream_t)hip_stream;
+    LRD_TRY((dt == LRD_BF16 ? block_norm_bwd_bf16 : block_norm_bwd_f32)(g, st));
+    LRD_TRY(block_norm_sums(g, outs, st));
     return LRD_OK;
 }
 

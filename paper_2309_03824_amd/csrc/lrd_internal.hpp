@@ -6,6 +6,7 @@
 
 #include "lrd_device.hpp"
 #include "once_per_device.hpp"
+#include "philox.hpp"
 
 namespace lrd {
 
@@ -177,6 +178,7 @@ void note_kernel(const char* name);
 // Elementwise / reductions.
 hipError_t gelu_fwd(const void* Z, void* A, int64_t n, bool bf16, hipStream_t st);
 hipError_t gelu_bwd(const void* dA, const void* Z, void* dZ, int64_t n, bool bf16, hipStream_t st);
+hipError_t dropout(const void* X, void* Y, int64_t n, bool bf16, const DropRng& rng, hipStream_t st);
 // out[c] = sum over t of dY[t][c]; `scratch` (optional) holds partial rows, fewer of them if it is small.
 // column_sum_rows: rows of dY to a partial row; *partials of them.
 int64_t column_sum_rows(const void* dY, int64_t T, int64_t n, bool bf16, size_t scratch_bytes, int64_t* partials);

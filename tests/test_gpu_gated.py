@@ -1,0 +1,194 @@
+"""Gated pairs against 64 bits.  Every intermediate that the library stores (H, dZ, dH) is compared by itself, and what follows is
+computed from the stored one: the bounds are then those of one product and one rounding (block_ref.py)."""
+import pytest
+import torch
+
+import block_ref as ref
+from parity import workspace
+from paper_2309_03824_amd import binding as lrd
+
+pytestmark = pytest.mark.gpu
+TYPES = {"bf16": torch.bfloat16, "f32": torch.float32}
+CODE = {"bf16": lrd.BF16, "f32": lrd.F32}
+
+
+def inputs(T, n_in, n_out, r, dt, bias, seed=0, scale=1.0):
+    g = torch.Generator().manual_seed(seed)
+    td = TYPES[dt]
+    rand = lambda *s, std=1.0: (torch.randn(*s, generator=g) * std).to(td).cuda()
+    X, V = rand(T, n_in), rand(2 * r, n_in, std=n_in ** -0.5)
+    Uc, dA = rand(2, n_out, r, std=scale * r ** -0.5), rand(T, n_out, std=0.1)
+    b = (torch.randn(2, n_out, generator=g) * 0.3).cuda() if bias else None
+    return X, V, Uc, b, dA
+
+
+def host(t):
+    return None if t is None else t.cpu().double()
+
+
+def guarded(*shape, dt, fill):
+    """A tensor with a row of sentinels behind it, as a view of one allocation."""
+    n = 1
+    for s in shape:
+        n *= s
+    flat = torch.full((n + 64,), fill, dtype=dt, device="cuda")
+    return flat[:n].view(*shape), flat[n:]
+
+
+SHAPES = [(1, 16, 16, 8), (1, 1024, 4096, 256), (2, 7, 5, 3), (3, 64, 1, 1), (17, 33, 65, 31), (31, 72, 200, 24), (64, 64, 64, 64), (65, 128, 129, 64), (129, 104, 136, 37),
+          (300, 256, 520, 100), (257, 520, 264, 257), (1030, 512, 2048, 256), (2100, 768, 1536, 208), (700, 600, 3000, 515)]
+
+
+@pytest.mark.parametrize("act", [lrd.ACT_NONE, lrd.ACT_GELU, lrd.ACT_SILU])
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+@pytest.mark.parametrize("T,n_in,n_out,r", SHAPES)
+def test_gated_against_64_bits(T, n_in, n_out, r, dt, act):
+    r = min(r, n_in, n_out)
+    td, bias = TYPES[dt], (T + act) % 2 == 0
+    X, V, Uc, b, dA = inputs(T, n_in, n_out, r, dt, bias, seed=T + act)
+    ws = workspace(lrd.linear_gated_workspace_bytes(T, n_in, n_out, r, CODE[dt]))
+    A, behind = guarded(T, n_out, dt=td, fill=77.0)
+    H, behind_h = guarded(T, 2 * r, dt=td, fill=77.0)
+    lrd.linear_gated_fwd(X, V, Uc, b, A, H, act, ws)
+    A2 = torch.empty_like(A)
+    lrd.linear_gated_fwd(X, V, Uc, b, A2, None, act, ws)
+    hX, hV, hU, hb, hdA, hH = (host(t) for t in (X, V, Uc, b, dA, H))
+    h, eh = ref.product(hX, hV)
+    ref.assert_close(H, (h, ref.SAFE * eh), td, "H")
+    ref.assert_close(A, ref.gated(hH, hU, hb, act, td), td, "A")
+    assert torch.equal(A, A2)
+    assert (behind == 77).all() and (behind_h == 77).all()
+
+    # the data gradient
+    dX, dZ, dH = torch.empty_like(X), torch.empty(2, T, n_out, dtype=td, device="cuda"), torch.empty(T, 2 * r, dtype=td, device="cuda")
+    lrd.linear_gated_bwd_data(dA, H, V, Uc, b, dX, dZ, dH, act, ws)
+    for k, want in enumerate(ref.gated(hH, hU, hb, act, td, hdA)):
+        ref.assert_close(dZ[k], want, td, "dZ")
+    hZ, hdH = host(dZ), host(dH)
+    for k in range(2):
+        c, e = ref.product(hZ[k], hU[k].t())
+        ref.assert_close(dH[:, k * r:(k + 1) * r].contiguous(), (c, ref.SAFE * e), td, "dH")
+    c, e = ref.product(hdH, hV.t())
+    ref.assert_close(dX, (c, ref.SAFE * e), td, "dX")
+
+    # all gradients in one call: the same data gradient, weight gradients from the same dZ and dH
+    f = lambda *s: torch.full(s, 9.0, device="cuda")
+    gX, gV, gU, gb = torch.empty_like(X), f(2 * r, n_in), f(2, n_out, r), f(2, n_out)
+    lrd.linear_gated_bwd(dA, X, H, V, Uc, b, gX, gV, gU, gb, 0, act, ws)
+    ref.assert_close(gX, (c, ref.SAFE * e), td, "dX")
+    for k in range(2):
+        c, e = ref.product(hZ[k].t(), hH[:, k * r:(k + 1) * r].t())
+        ref.assert_close(gU[k], (c, ref.SAFE * e), torch.float32, "dU")
+        ref.assert_close(gb[k], (hZ[k].sum(0), ref.SAFE * (T + 2) * ref.U * hZ[k].abs().sum(0)), torch.float32, "dbias")
+    c, e = ref.product(hdH.t(), hX.t())
+    if dt == "bf16" and r % 8 and n_in % 8 == 0 and n_out % 8 == 0:
+        # at a padded rank the data gradients are in the same order too
+        assert torch.equal(gX, dX)
+    ref.assert_close(gV, (c, ref.SAFE * e), torch.float32, "dV")
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+@pytest.mark.parametrize("r", [24, 29])
+def test_frozen_factors_and_null_arguments(dt, r):
+    T, n_in, n_out, act = 77, 64, 96, lrd.ACT_SILU
+    X, V, Uc, b, dA = inputs(T, n_in, n_out, r, dt, True)
+    td = TYPES[dt]
+    ws = workspace(lrd.linear_gated_workspace_bytes(T, n_in, n_out, r, CODE[dt]))
+    H = torch.empty(T, 2 * r, dtype=td, device="cuda")
+    lrd.linear_gated_fwd(X, V, Uc, b, torch.empty(T, n_out, dtype=td, device="cuda"), H, act, ws)
+    f = lambda *s: torch.full(s, 9.0, device="cuda")
+
+    def grads(mask, H=H, X=X, want_x=True, want_b=True):
+        out = dict(dX=torch.full((T, n_in), 9.0, dtype=td, device="cuda"), dV=f(2 * r, n_in), dU=f(2, n_out, r), db=f(2, n_out))
+        lrd.linear_gated_bwd(dA, X, H, V, Uc, b, out["dX"] if want_x else None, out["dV"], out["dU"], out["db"] if want_b else None, mask, act, ws)
+        return out
+    whole = grads(0)
+    for mask, frozen in ((1, {"dV"}), (2, {"dU"}), (3, {"dV", "dU"})):
+        got = grads(mask)
+        for k, v in got.items():
+            assert (v == 9).all() if k in frozen else torch.equal(v, whole[k]), (mask, k)
+    again = grads(0, H=None)            # H from X: the forward's product
+    assert all(torch.equal(again[k], whole[k]) for k in whole)
+    no_x = grads(0, want_x=False, want_b=False)
+    assert (no_x["dX"] == 9).all() and (no_x["db"] == 9).all() and torch.equal(no_x["dV"], whole["dV"]) and torch.equal(no_x["dU"], whole["dU"])
+    frozen = grads(1, X=None)           # a frozen first factor with H needs no X
+    assert torch.equal(frozen["dX"], whole["dX"]) and torch.equal(frozen["dU"], whole["dU"])
+
+
+def test_batched_weight_gradients_of_a_gated_pair():
+    """dZ and dH of the data gradient go into lrd_linear_wgrad_batched as a stack's backward puts them there."""
+    T, n_in, n_out, r, L, act = 264, 128, 192, 32, 3, lrd.ACT_GELU
+    parts = [inputs(T, n_in, n_out, r, "bf16", False, seed=l) for l in range(L)]
+    bf = dict(dtype=torch.bfloat16, device="cuda")
+    Xs, H, dH, dZ = torch.stack([p[0] for p in parts]), torch.empty(L, T, 2 * r, **bf), torch.empty(L, T, 2 * r, **bf), torch.empty(L, 2, T, n_out, **bf)
+    ws = workspace(max(lrd.linear_gated_workspace_bytes(T, n_in, n_out, r, lrd.BF16),
+                       lrd.linear_wgrad_batched_workspace_bytes(L, T, n_in, n_out, 2 * r, lrd.BF16)))
+    dX = torch.empty(T, n_in, **bf)
+    for l, (X, V, Uc, _, dA) in enumerate(parts):
+        lrd.linear_gated_fwd(X, V, Uc, None, torch.empty(T, n_out, **bf), H[l], act, ws)
+        lrd.linear_gated_bwd_data(dA, H[l], V, Uc, None, dX, dZ[l], dH[l], act, ws)
+    dV, dU = torch.empty(L, 2 * r, n_in, device="cuda"), torch.empty(2, L, n_out, r, device="cuda")
+    lrd.linear_wgrad_batched(None, None, dH, Xs, dV, None, lrd.FREEZE_L1, ws)
+    for k in range(2):
+        lrd.linear_wgrad_batched(dZ[:, k], H[:, :, k * r:(k + 1) * r], None, None, None, dU[k], lrd.FREEZE_L0, ws)
+    for l, (X, V, Uc, _, dA) in enumerate(parts):
+        c, e = ref.product(host(dH[l]).t(), host(X).t())
+        ref.assert_close(dV[l], (c, ref.SAFE * e), torch.float32, "dV")
+        for k in range(2):
+            c, e = ref.product(host(dZ[l, k]).t(), host(H[l][:, k * r:(k + 1) * r]).t())
+            ref.assert_close(dU[k, l], (c, ref.SAFE * e), torch.float32, "dU")
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+@pytest.mark.parametrize("act", [lrd.ACT_GELU, lrd.ACT_SILU])
+def test_saturated_gates(dt, act):
+    """Gates far out on both sides: act runs into 0 and z, its derivative into 0 and 1; nothing overflows."""
+    T, n_in, n_out, r = 70, 64, 128, 16
+    X, V, Uc, b, dA = inputs(T, n_in, n_out, r, dt, True, scale=60.0)
+    td = TYPES[dt]
+    ws = workspace(lrd.linear_gated_workspace_bytes(T, n_in, n_out, r, CODE[dt]))
+    A, H, dZ, dH = (torch.empty(*s, dtype=td, device="cuda") for s in ((T, n_out), (T, 2 * r), (2, T, n_out), (T, 2 * r)))
+    lrd.linear_gated_fwd(X, V, Uc, b, A, H, act, ws)
+    lrd.linear_gated_bwd_data(dA, H, V, Uc, b, None, dZ, dH, act, ws)
+    zg = host(H)[:, :r] @ host(Uc)[0].t()
+    assert zg.max() > 90 and zg.min() < -90
+    ref.assert_close(A, ref.gated(host(H), host(Uc), host(b), act, td), td, "A")
+    for k, want in enumerate(ref.gated(host(H), host(Uc), host(b), act, td, host(dA))):
+        ref.assert_close(dZ[k], want, td, "dZ")
+
+
+def test_gated_replays_and_runs_on_another_stream():
+    T, n_in, n_out, r, act = 520, 256, 512, 64, lrd.ACT_SILU
+    X, V, Uc, b, dA = inputs(T, n_in, n_out, r, "bf16", True)
+    bf = dict(dtype=torch.bfloat16, device="cuda")
+    A, H, dX = torch.empty(T, n_out, **bf), torch.empty(T, 2 * r, **bf), torch.empty(T, n_in, **bf)
+    dV, dU, db = torch.empty(2 * r, n_in, device="cuda"), torch.empty(2, n_out, r, device="cuda"), torch.empty(2, n_out, device="cuda")
+    ws = workspace(lrd.linear_gated_workspace_bytes(T, n_in, n_out, r, lrd.BF16))
+    outs = [A, H, dX, dV, dU, db]
+
+    def step():
+        lrd.linear_gated_fwd(X, V, Uc, b, A, H, act, ws)
+        lrd.linear_gated_bwd(dA, X, H, V, Uc, b, dX, dV, dU, db, 0, act, ws)
+    step()
+    torch.cuda.synchronize()
+    want = [t.clone() for t in outs]
+    side, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        step()
+    for rep in range(3):
+        for t in outs:
+            t.fill_(float(rep))
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(t, w) for t, w in zip(outs, want)), rep
+        step()
+        torch.cuda.synchronize()
+        assert all(torch.equal(t, w) for t, w in zip(outs, want)), rep
+    for t in outs:
+        t.zero_()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step()
+    side.synchronize()
+    assert all(torch.equal(t, w) for t, w in zip(outs, want))
