@@ -153,8 +153,10 @@ hipError_t launch(const MatOp& op, int splits, hipStream_t st)
 bool f32_gemm_supported(const MatOp& op)
 {
     if (op.in_bf16 || !op.out_f32 || op.gather != GATHER_NONE || op.batch != 1) return false;
-    // A K-major operand is read in pairs of rows: a single token and rank 1 stay with the FMA engine.
-    if (op.M < 2 || op.N < 2 || op.K < 1) return false;
+    // A K-major operand is read in pairs of rows: a single token and rank 1 stay with the FMA engine.  A single row that is contiguous along K
+    // need not, and goes here where the caller says so (all gradients of one token of a gated pair 768 -> 2056 at rank 134 511 us there, 34 us
+    // here); the layers' own passes keep that engine's bits.
+    if (op.M < (op.one_row && op.a_sk == 1 ? 1 : 2) || op.N < 2 || op.K < 1) return false;
     const int64_t lim = int64_t(1) << 30;
     if (op.M >= lim || op.N >= lim || op.K >= lim || ceil_div(op.N, 16) > 65535) return false;
     return (op.a_sk == 1 || op.a_sm == 1) && (op.b_sk == 1 || op.b_sn == 1);

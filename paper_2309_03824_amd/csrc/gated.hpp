@@ -6,16 +6,19 @@
 namespace lrd {
 
 // Zg = Hg.Ug^T + bg, Zu = Hu.Uu^T + bu from H = [Hg | Hu] [T x 2 r], U [2][out x r], bias [2][out] or null;
-// forward (dA null): A = act(Zg) * Zu;  backward: dZ[0] = dA * Zu * act'(Zg), dZ[1] = dA * act(Zg).
+// forward (dA null): A = act(Zg) * Zu;  backward: dZ[0] = dA * Zu * act'(Zg), dZ[1] = dA * act(Zg), in rows of ldz = out elements or
+// out rounded up to a multiple of 8, then padded with zeros.
 struct GatedOp {
     const void *H, *U;
     const float* bias;
     const void* dA;
-    void *A, *dZ;               // dZ [2][T x out]
-    int64_t T, out, r;
+    void *A, *dZ;               // dZ [2][T x ldz]
+    int64_t T, out, r, ldz, u_rows;     // u_rows: of each factor in U, out or as padded
     int act;                    // lrd.h's LRD_ACT_*
     bool bf16;
 };
 hipError_t run_gated(const GatedOp& op, hipStream_t st);
+// dst [2][rows x cols] = the first rows and columns of src [2][rows_s x cols_s] (fp32).
+hipError_t crop_pair(const float* src, int64_t rows_s, int64_t cols_s, float* dst, int64_t rows, int64_t cols, hipStream_t st);
 
 }  // namespace lrd

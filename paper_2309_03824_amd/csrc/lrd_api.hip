@@ -650,9 +650,10 @@ lrd_status lrd_linear_group_fwd(const void* X, const void* V_cat, const void* U,
     return LRD_OK;
 }
 
-lrd_status lrd_linear_group_bwd(const void* dY, const void* X, const void* H, const void* V_cat, const void* U, void* dX,
-                                float* dV_cat, float* dU, float* dbias, uint32_t freeze_mask, int64_t T, int64_t in, int64_t out,
-                                int64_t r, int32_t groups, lrd_dtype dt, void* ws, size_t ws_bytes, void* hip_stream)
+namespace {
+lrd_status group_bwd(const void* dY, const void* X, const void* H, const void* V_cat, const void* U, void* dX, float* dV_cat, float* dU,
+                     float* dbias, uint32_t freeze_mask, int64_t T, int64_t in, int64_t out, int64_t r, int32_t groups, lrd_dtype dt, void* ws,
+                     size_t ws_bytes, void* hip_stream, bool one_row)
 {
     if (!dtype_ok(dt) || !group_dims_ok(T, in, out, r, groups) || !dY || !V_cat || !U) return LRD_ERR_INVALID_ARG;
     if (freeze_mask & ~uint32_t(LRD_FREEZE_L0 | LRD_FREEZE_L1)) return LRD_ERR_INVALID_ARG;
@@ -680,12 +681,14 @@ lrd_status lrd_linear_group_bwd(const void* dY, const void* X, const void* H, co
                 MatOp d1 = nn(at(dY, (int64_t)g * T * out, dt), out, at(U, (int64_t)g * out * r, dt), r, (void*)at(dH, g * r, dt), gr,
                               T, r, out, dt);
                 d1.role = LRD_ROLE_DGRAD_UP;
+                d1.one_row = one_row;
                 share_splits(d1, region, dt, SPLIT_ACT);
                 LRD_TRY(run_matop(d1, st));
             }
         } else {
             MatOp d1 = nn(dY, out, U, r, dH, gr, T, r, out, dt);
             d1.role = LRD_ROLE_DGRAD_UP;
+            d1.one_row = one_row;
             d1.batch = groups;
             d1.a_bs = T * out; d1.b_bs = out * r; d1.c_bs = r;
             LRD_TRY(run_matop(d1, st));
@@ -693,6 +696,7 @@ lrd_status lrd_linear_group_bwd(const void* dY, const void* X, const void* H, co
         if (dX) {
             MatOp d2 = nn(dH, gr, V_cat, in, dX, in, T, in, gr, dt);
             d2.role = LRD_ROLE_DGRAD_DOWN;
+            d2.one_row = one_row;
             LRD_TRY(run_matop(d2, st));
         }
     }
@@ -722,6 +726,14 @@ lrd_status lrd_linear_group_bwd(const void* dY, const void* X, const void* H, co
         for (int32_t g = 0; g < groups; ++g)
             LRD_TRY(column_sums(at(dY, (int64_t)g * T * out, dt), dbias + (int64_t)g * out, T, out, dt == LRD_BF16, ws, cv.used, st));
     return LRD_OK;
+}
+}  // namespace
+
+lrd_status lrd_linear_group_bwd(const void* dY, const void* X, const void* H, const void* V_cat, const void* U, void* dX,
+                                float* dV_cat, float* dU, float* dbias, uint32_t freeze_mask, int64_t T, int64_t in, int64_t out,
+                                int64_t r, int32_t groups, lrd_dtype dt, void* ws, size_t ws_bytes, void* hip_stream)
+{
+    return group_bwd(dY, X, H, V_cat, U, dX, dV_cat, dU, dbias, freeze_mask, T, in, out, r, groups, dt, ws, ws_bytes, hip_stream, false);
 }
 
 // ------------------------------------------------------------------------------------ deferred weight gradients
@@ -756,9 +768,9 @@ lrd_status lrd_linear_bwd_data(const void* dY, const void* V, const void* U, voi
     return LRD_OK;
 }
 
-lrd_status lrd_linear_group_bwd_data(const void* dY, const void* V_cat, const void* U, void* dX, void* dH_save, int64_t T,
-                                     int64_t in, int64_t out, int64_t r, int32_t groups, lrd_dtype dt, void* ws,
-                                     size_t ws_bytes, void* hip_stream)
+namespace {
+lrd_status group_bwd_data(const void* dY, const void* V_cat, const void* U, void* dX, void* dH_save, int64_t T, int64_t in, int64_t out, int64_t r,
+                          int32_t groups, lrd_dtype dt, void* ws, size_t ws_bytes, void* hip_stream, bool one_row)
 {
     if (!dtype_ok(dt) || !group_dims_ok(T, in, out, r, groups) || !dY || !V_cat || !U || !dH_save) return LRD_ERR_INVALID_ARG;
     if (!aligned16(dY) || !aligned16(V_cat) || !aligned16(U) || !aligned16(dX) || !aligned16(dH_save) || !aligned16(ws))
@@ -774,12 +786,14 @@ lrd_status lrd_linear_group_bwd_data(const void* dY, const void* V_cat, const vo
             MatOp d1 = nn(at(dY, (int64_t)g * T * out, dt), out, at(U, (int64_t)g * out * r, dt), r, (void*)at(dH_save, g * r, dt),
                           gr, T, r, out, dt);
             d1.role = LRD_ROLE_DGRAD_UP;
+            d1.one_row = one_row;
             share_splits(d1, region, dt, SPLIT_ACT);
             LRD_TRY(run_matop(d1, st));
         }
     } else {
         MatOp d1 = nn(dY, out, U, r, dH_save, gr, T, r, out, dt);
         d1.role = LRD_ROLE_DGRAD_UP;
+        d1.one_row = one_row;
         d1.batch = groups;
         d1.a_bs = T * out; d1.b_bs = out * r; d1.c_bs = r;
         LRD_TRY(run_matop(d1, st));
@@ -787,9 +801,18 @@ lrd_status lrd_linear_group_bwd_data(const void* dY, const void* V_cat, const vo
     if (dX) {
         MatOp d2 = nn(dH_save, gr, V_cat, in, dX, in, T, in, gr, dt);
         d2.role = LRD_ROLE_DGRAD_DOWN;
+        d2.one_row = one_row;
         LRD_TRY(run_matop(d2, st));
     }
     return LRD_OK;
+}
+}  // namespace
+
+lrd_status lrd_linear_group_bwd_data(const void* dY, const void* V_cat, const void* U, void* dX, void* dH_save, int64_t T,
+                                     int64_t in, int64_t out, int64_t r, int32_t groups, lrd_dtype dt, void* ws,
+                                     size_t ws_bytes, void* hip_stream)
+{
+    return group_bwd_data(dY, V_cat, U, dX, dH_save, T, in, out, r, groups, dt, ws, ws_bytes, hip_stream, false);
 }
 
 namespace {
@@ -865,38 +888,78 @@ lrd_status lrd_linear_wgrad_batched(const void* dY, int64_t dy_stride, const voi
 namespace {
 inline bool act_ok(int32_t act) { return act == LRD_ACT_NONE || act == LRD_ACT_GELU || act == LRD_ACT_SILU; }
 
-// What lrd_linear_group_bwd takes of its workspace for two layers with H given.
-size_t gated_group_bytes(int64_t T, int64_t in, int64_t out, int64_t r, lrd_dtype dt, bool need_dH, Tokens tokens)
+// A gated pair whose rank or outputs are no multiple of 8 (bf16) is computed at the padded sizes on zero-padded copies, as a single layer's raw
+// rank is; dZ, which lies in the workspace, gets padded rows.  All gradients of 4762 x 768 -> 1001 at rank 320: 398 us on the kernels for
+// any alignment, 108 us padded.
+struct GatedSizes {
+    int64_t r, out;         // of the products
+    bool pad_r, pad_out;
+};
+GatedSizes gated_sizes(int64_t in, int64_t out, int64_t r, lrd_dtype dt)
 {
-    return (need_dH ? round256((size_t)T * 2 * r * esize(dt)) : 0) + round256(group_partial_region(T, in, out, r, 2, dt, true, tokens));
+    const bool pads = dt == LRD_BF16 && in % 8 == 0;
+    GatedSizes z{pads ? pad8(r) : r, pads ? pad8(out) : out, false, false};
+    z.pad_r = z.r != r;
+    z.pad_out = z.out != out;
+    return z;
 }
-// Padded copies of U, V_cat and H, and, for a whole backward, of dU and dV_cat.
-size_t gated_pad_bytes(int64_t T, int64_t in, int64_t out, int64_t r8, bool grads)
+
+// What lrd_linear_group_bwd takes of its workspace for two layers with H given.
+size_t gated_group_bytes(int64_t T, int64_t in, const GatedSizes& z, lrd_dtype dt, bool need_dH, Tokens tokens)
 {
-    return round256((size_t)2 * out * r8 * 2) + round256((size_t)2 * r8 * in * 2) + round256((size_t)T * 2 * r8 * 2) +
-           (grads ? round256((size_t)2 * out * r8 * 4) + round256((size_t)2 * r8 * in * 4) : 0);
+    return (need_dH ? round256((size_t)T * 2 * z.r * esize(dt)) : 0) + round256(group_partial_region(T, in, z.out, z.r, 2, dt, true, tokens));
 }
 
 GatedOp gated_op(const void* H, const void* U, const float* bias, int64_t T, int64_t out, int64_t r, int32_t act, lrd_dtype dt)
 {
     GatedOp op{};
     op.H = H; op.U = U; op.bias = bias;
-    op.T = T; op.out = out; op.r = r; op.act = act; op.bf16 = dt == LRD_BF16;
+    op.T = T; op.out = op.ldz = op.u_rows = out; op.r = r; op.act = act; op.bf16 = dt == LRD_BF16;
     return op;
 }
-// Zero-padded copies of a group of two's factors and intermediate at rank r8 (any of them null).
-hipError_t pad_gated(const void* U, void* Up, const void* V, void* Vp, const void* H, void* Hp, int64_t T, int64_t in, int64_t out, int64_t r,
-                     int64_t r8, hipStream_t st)
-{
-    CopyJob jobs[4];
+
+// Zero-padded copies of a gated pair's operands at its padded sizes, in the workspace; what needs none stays where it is.
+struct GatedPadded {
+    const void *U, *V, *H;
+    CopyJob jobs[5];
     int n = 0;
-    if (U) jobs[n++] = {U, 2 * out, r, Up, 2 * out, r8, 2};
-    if (V) {
-        jobs[n++] = {V, r, in, Vp, r8, in, 2};
-        jobs[n++] = {(const char*)V + r * in * 2, r, in, (char*)Vp + r8 * in * 2, r8, in, 2};
+
+    GatedPadded(const void* U_, const void* V_, const void* H_) : U(U_), V(V_), H(H_) {}
+    void factors(Carver& cv, int64_t in, int64_t out, int64_t r, int64_t out_to, int64_t r_to)
+    {
+        if (out_to != out || r_to != r) {
+            char* Up = (char*)cv.take((size_t)2 * out_to * r_to * 2);
+            if (out_to == out) jobs[n++] = {U, 2 * out, r, Up, 2 * out, r_to, 2};
+            else {
+                jobs[n++] = {U, out, r, Up, out_to, r_to, 2};
+                jobs[n++] = {(const char*)U + out * r * 2, out, r, Up + out_to * r_to * 2, out_to, r_to, 2};
+            }
+            U = Up;
+        }
+        if (r_to != r) {
+            char* Vp = (char*)cv.take((size_t)2 * r_to * in * 2);
+            jobs[n++] = {V, r, in, Vp, r_to, in, 2};
+            jobs[n++] = {(const char*)V + r * in * 2, r, in, Vp + r_to * in * 2, r_to, in, 2};
+            V = Vp;
+        }
     }
-    if (H) jobs[n++] = {H, 2 * T, r, Hp, 2 * T, r8, 2};
-    return copy2d(jobs, n, st);
+    void* intermediate(Carver& cv, int64_t T, int64_t r, int64_t r_to)      // its copy, where there is one
+    {
+        void* Hp = cv.take((size_t)T * 2 * r_to * 2);
+        jobs[n++] = {H, 2 * T, r, Hp, 2 * T, r_to, 2};
+        H = Hp;
+        return Hp;
+    }
+};
+size_t gated_factor_bytes(int64_t in, const GatedSizes& z)
+{
+    return (z.pad_r || z.pad_out ? round256((size_t)2 * z.out * z.r * 2) : 0) + (z.pad_r ? round256((size_t)2 * z.r * in * 2) : 0);
+}
+// Of fp32 gradients at padded sizes, cropped at the end.
+size_t gated_grad_bytes(int64_t in, const GatedSizes& z)
+{
+    return (z.pad_r || z.pad_out ? round256((size_t)2 * z.out * z.r * 4) : 0) + (z.pad_r ? round256((size_t)2 * z.r * in * 4) : 0) +
+           (z.pad_out ? round256((size_t)2 * z.out * 4) : 0);
 }
 }  // namespace
 
@@ -904,13 +967,12 @@ size_t lrd_linear_gated_workspace_bytes(int64_t T, int64_t in, int64_t out, int6
 {
     (void)freeze_mask;
     if (!dtype_ok(dt) || !group_dims_ok(T, in, out, r, 2)) return 0;
-    const bool pads = pads_rank(in, out, r, dt);
-    const int64_t rr = pads ? pad8(r) : r;
-    const size_t H = round256((size_t)T * 2 * rr * esize(dt)), dZ = round256((size_t)2 * T * out * esize(dt));
-    const size_t fwd = H + round256(group_partial_region(T, in, out, rr, 2, dt, false, UP_TO));
-    const size_t bwd = dZ + H + gated_group_bytes(T, in, out, rr, dt, true, UP_TO);
-    const size_t data = H + round256(act_partial_bytes(T, rr, out, dt, UP_TO));
-    return std::max(std::max(fwd, bwd), data) + (pads ? gated_pad_bytes(T, in, out, rr, true) : 0);
+    const GatedSizes z = gated_sizes(in, out, r, dt);
+    const size_t H = round256((size_t)T * 2 * z.r * esize(dt)), dZ = round256((size_t)2 * T * z.out * esize(dt)), pads = gated_factor_bytes(in, z);
+    const size_t fwd = pads + H + round256(group_partial_region(T, in, out, z.r, 2, dt, false, UP_TO));
+    const size_t bwd = pads + gated_grad_bytes(in, z) + dZ + H + gated_group_bytes(T, in, z, dt, true, UP_TO);
+    const size_t data = pads + H + (z.pad_out ? dZ : 0) + round256(act_partial_bytes(T, z.r, z.out, dt, UP_TO));
+    return std::max(std::max(fwd, bwd), data);
 }
 
 lrd_status lrd_linear_gated_fwd(const void* X, const void* V_cat, const void* U, const float* bias, void* A, void* H_save, int32_t act,
@@ -920,28 +982,25 @@ lrd_status lrd_linear_gated_fwd(const void* X, const void* V_cat, const void* U,
     if (!aligned16(X) || !aligned16(V_cat) || !aligned16(U) || !aligned16(bias) || !aligned16(A) || !aligned16(H_save) || !aligned16(ws))
         return LRD_ERR_ALIGNMENT;
     hipStream_t st = (hipStream_t)hip_stream;
-    const bool pads = pads_rank(in, out, r, dt);
-    const int64_t rr = pads ? pad8(r) : r;
+    const GatedSizes z = gated_sizes(in, out, r, dt);
     Carver cv(ws, ws_bytes);
-    void *Up = nullptr, *Vp = nullptr;
-    if (pads) {
-        Up = cv.take((size_t)2 * out * rr * 2);
-        Vp = cv.take((size_t)2 * rr * in * 2);
-    }
-    void* H = H_save && !pads ? H_save : cv.take((size_t)T * 2 * rr * esize(dt));
-    const size_t region_bytes = group_partial_region(T, in, out, rr, 2, dt, false);
+    GatedPadded p(U, V_cat, nullptr);
+    p.factors(cv, in, out, r, out, z.r);
+    void* H = H_save && !z.pad_r ? H_save : cv.take((size_t)T * 2 * z.r * esize(dt));
+    const size_t region_bytes = group_partial_region(T, in, out, z.r, 2, dt, false);
     void* region = region_bytes ? cv.take(region_bytes) : nullptr;
     if (!cv.ok) return LRD_ERR_WORKSPACE;
-    if (pads) LRD_TRY(pad_gated(U, Up, V_cat, Vp, nullptr, nullptr, T, in, out, r, rr, st));
-    MatOp g1 = nt(X, in, pads ? Vp : V_cat, in, H, 2 * rr, T, 2 * rr, in, dt, false);
+    LRD_TRY(copy2d(p.jobs, p.n, st));
+    MatOp g1 = nt(X, in, p.V, in, H, 2 * z.r, T, 2 * z.r, in, dt, false);
     g1.role = LRD_ROLE_FWD_DOWN;
+    g1.one_row = true;
     share_splits(g1, region, dt, SPLIT_ACT);
     LRD_TRY(run_matop(g1, st));
-    GatedOp op = gated_op(H, pads ? Up : U, bias, T, out, rr, act, dt);
+    GatedOp op = gated_op(H, p.U, bias, T, out, z.r, act, dt);
     op.A = A;
     LRD_TRY(run_gated(op, st));
-    const CopyJob crop = {H, 2 * T, rr, H_save, 2 * T, r, 2};
-    if (pads && H_save) LRD_TRY(copy2d(&crop, 1, st));
+    const CopyJob crop = {H, 2 * T, z.r, H_save, 2 * T, r, 2};
+    if (z.pad_r && H_save) LRD_TRY(copy2d(&crop, 1, st));
     return LRD_OK;
 }
 
@@ -959,42 +1018,36 @@ lrd_status lrd_linear_gated_bwd(const void* dA, const void* X, const void* H, co
     hipStream_t st = (hipStream_t)hip_stream;
     const bool need_dH = dX || train_v;
     if (!need_dH && !train_u && !dbias) return LRD_OK;
-    const bool pads = pads_rank(in, out, r, dt);
-    const int64_t rr = pads ? pad8(r) : r;
+    const GatedSizes z = gated_sizes(in, out, r, dt);
     Carver cv(ws, ws_bytes);
-    void *Up = nullptr, *Vp = nullptr, *dUp = nullptr, *dVp = nullptr;
-    if (pads) {
-        Up = cv.take((size_t)2 * out * rr * 2);
-        Vp = cv.take((size_t)2 * rr * in * 2);
-        dUp = train_u ? cv.take((size_t)2 * out * rr * 4) : nullptr;
-        dVp = train_v ? cv.take((size_t)2 * rr * in * 4) : nullptr;
-    }
-    void* Hw = !H || pads ? cv.take((size_t)T * 2 * rr * esize(dt)) : nullptr;
-    void* dZ = cv.take((size_t)2 * T * out * esize(dt));
-    const size_t rest = gated_group_bytes(T, in, out, rr, dt, need_dH, THESE);
+    GatedPadded p(U, V_cat, H);
+    p.factors(cv, in, out, r, z.out, z.r);
+    float* const gU = train_u && (z.pad_r || z.pad_out) ? (float*)cv.take((size_t)2 * z.out * z.r * 4) : dU;
+    float* const gV = train_v && z.pad_r ? (float*)cv.take((size_t)2 * z.r * in * 4) : dV_cat;
+    float* const gb = dbias && z.pad_out ? (float*)cv.take((size_t)2 * z.out * 4) : dbias;
+    void* Hnew = nullptr;
+    if (!H) p.H = Hnew = cv.take((size_t)T * 2 * z.r * esize(dt));
+    else if (z.pad_r) p.intermediate(cv, T, r, z.r);
+    void* dZ = cv.take((size_t)2 * T * z.out * esize(dt));
+    const size_t rest = gated_group_bytes(T, in, z, dt, need_dH, THESE);
     char* const rest_at = (char*)ws + cv.used;
     if (!cv.ok || (rest && !cv.room(rest))) return LRD_ERR_WORKSPACE;
-    if (pads) LRD_TRY(pad_gated(U, Up, V_cat, Vp, H, Hw, T, in, out, r, rr, st));
-    const void *Vc = pads ? Vp : V_cat, *Uc = pads ? Up : U, *Hc = Hw ? Hw : H;
-    if (!H) {
-        MatOp re = nt(X, in, Vc, in, Hw, 2 * rr, T, 2 * rr, in, dt, false);
+    LRD_TRY(copy2d(p.jobs, p.n, st));
+    if (Hnew) {
+        MatOp re = nt(X, in, p.V, in, Hnew, 2 * z.r, T, 2 * z.r, in, dt, false);
+        re.one_row = true;
         share_splits(re, rest_at, dt, SPLIT_ACT);          // (the group's region holds it: its first product comes later)
         LRD_TRY(run_matop(re, st));
     }
-    GatedOp op = gated_op(Hc, Uc, bias, T, out, rr, act, dt);
-    op.dA = dA; op.dZ = dZ;
+    GatedOp op = gated_op(p.H, p.U, bias, T, out, z.r, act, dt);
+    op.dA = dA; op.dZ = dZ; op.ldz = op.u_rows = z.out;
     LRD_TRY(run_gated(op, st));
-    const lrd_status rc = lrd_linear_group_bwd(dZ, X, Hc, Vc, Uc, dX, pads ? (float*)dVp : dV_cat, pads ? (float*)dUp : dU, dbias, freeze_mask, T, in,
-                                               out, rr, 2, dt, rest_at, ws_bytes - cv.used, hip_stream);
-    if (rc != LRD_OK || !pads) return rc;
-    CopyJob crops[3];
-    int n = 0;
-    if (train_u) crops[n++] = {dUp, 2 * out, rr, dU, 2 * out, r, 4};
-    if (train_v) {
-        crops[n++] = {dVp, r, in, dV_cat, r, in, 4};
-        crops[n++] = {(const char*)dVp + rr * in * 4, r, in, (char*)dV_cat + r * in * 4, r, in, 4};
-    }
-    LRD_TRY(copy2d(crops, n, st));
+    const lrd_status rc = group_bwd(dZ, X, p.H, p.V, p.U, dX, gV, gU, gb, freeze_mask, T, in, z.out, z.r, 2, dt, rest_at, ws_bytes - cv.used, hip_stream, true);
+    if (rc != LRD_OK) return rc;
+    if (gU != dU) LRD_TRY(crop_pair(gU, z.out, z.r, dU, out, r, st));
+    if (gb != dbias) LRD_TRY(crop_pair(gb, z.out, 1, dbias, out, 1, st));
+    const CopyJob crops[2] = {{gV, r, in, dV_cat, r, in, 4}, {(const char*)gV + z.r * in * 4, r, in, (char*)dV_cat + r * in * 4, r, in, 4}};
+    if (gV != dV_cat) LRD_TRY(copy2d(crops, 2, st));
     return LRD_OK;
 }
 
@@ -1008,26 +1061,26 @@ lrd_status lrd_linear_gated_bwd_data(const void* dA, const void* H, const void* 
         !aligned16(dH_save) || !aligned16(ws))
         return LRD_ERR_ALIGNMENT;
     hipStream_t st = (hipStream_t)hip_stream;
-    const bool pads = pads_rank(in, out, r, dt);
-    const int64_t rr = pads ? pad8(r) : r;
+    const GatedSizes z = gated_sizes(in, out, r, dt);
     Carver cv(ws, ws_bytes);
-    void *Up = nullptr, *Vp = nullptr, *Hp = nullptr;
-    if (pads) {
-        Up = cv.take((size_t)2 * out * rr * 2);
-        Vp = cv.take((size_t)2 * rr * in * 2);
-        Hp = cv.take((size_t)T * 2 * rr * 2);          // H, and when dZ is made, dH
-    }
-    const size_t rest = act_partial_bytes(T, rr, out, dt);
+    GatedPadded p(U, V_cat, H);
+    p.factors(cv, in, out, r, z.out, z.r);
+    void* const Hp = z.pad_r ? p.intermediate(cv, T, r, z.r) : nullptr;        // H, and when dZ is made, dH
+    void* const gZ = z.pad_out ? cv.take((size_t)2 * T * z.out * esize(dt)) : dZ;
+    const size_t rest = act_partial_bytes(T, z.r, z.out, dt);
     if (!cv.ok || (rest && !cv.room(rest))) return LRD_ERR_WORKSPACE;
-    if (pads) LRD_TRY(pad_gated(U, Up, V_cat, Vp, H, Hp, T, in, out, r, rr, st));
-    GatedOp op = gated_op(pads ? Hp : H, pads ? Up : U, bias, T, out, rr, act, dt);
-    op.dA = dA; op.dZ = dZ;
+    LRD_TRY(copy2d(p.jobs, p.n, st));
+    GatedOp op = gated_op(p.H, p.U, bias, T, out, z.r, act, dt);
+    op.dA = dA; op.dZ = gZ; op.ldz = op.u_rows = z.out;
     LRD_TRY(run_gated(op, st));
-    const lrd_status rc = lrd_linear_group_bwd_data(dZ, pads ? Vp : V_cat, pads ? Up : U, dX, pads ? Hp : dH_save, T, in, out, rr, 2, dt,
-                                                    (char*)ws + cv.used, ws_bytes - cv.used, hip_stream);
-    if (rc != LRD_OK || !pads) return rc;
-    const CopyJob crop = {Hp, 2 * T, rr, dH_save, 2 * T, r, 2};
-    LRD_TRY(copy2d(&crop, 1, st));
+    const lrd_status rc = group_bwd_data(gZ, p.V, p.U, dX, Hp ? Hp : dH_save, T, in, z.out, z.r, 2, dt, (char*)ws + cv.used, ws_bytes - cv.used, hip_stream,
+                                         true);
+    if (rc != LRD_OK) return rc;
+    CopyJob crops[2];
+    int n = 0;
+    if (Hp) crops[n++] = {Hp, 2 * T, z.r, dH_save, 2 * T, r, 2};
+    if (gZ != dZ) crops[n++] = {gZ, 2 * T, z.out, dZ, 2 * T, out, 2};
+    LRD_TRY(copy2d(crops, n, st));
     return LRD_OK;
 }
 

@@ -98,6 +98,7 @@ struct MatOp {
     // Optional optimizer step on the finished fp32 result (a dense weight gradient, ldc == N).
     const SgdFuse* sgd = nullptr;
     const CropFuse* crop = nullptr;
+    bool one_row = false;          // fp32: a single row, contiguous along K, may go to the matrix cores too (see f32_gemm_supported)
     SumQueue* later = nullptr;     // where an engine may leave the sum over its K-slices (else it runs at once)
     // A batch of products of one shape (the layers of a group): product z reads A + z * a_bs,
     // B + z * b_bs, bias + z * bias_bs and writes C + z * c_bs, aux + z * aux_bs (element strides).

@@ -36,7 +36,7 @@ def guarded(*shape, dt, fill):
 
 
 SHAPES = [(1, 16, 16, 8), (1, 1024, 4096, 256), (2, 7, 5, 3), (3, 64, 1, 1), (17, 33, 65, 31), (31, 72, 200, 24), (64, 64, 64, 64), (65, 128, 129, 64), (129, 104, 136, 37),
-          (300, 256, 520, 100), (257, 520, 264, 257), (1030, 512, 2048, 256), (2100, 768, 1536, 208), (700, 600, 3000, 515)]
+          (300, 256, 520, 100), (257, 520, 264, 257), (1030, 512, 2048, 256), (2100, 768, 1536, 208), (700, 600, 3000, 515), (520, 1024, 1001, 320), (1100, 64, 1003, 64), (300, 1040, 1032, 520), (2, 512, 2730, 193)]
 
 
 @pytest.mark.parametrize("act", [lrd.ACT_NONE, lrd.ACT_GELU, lrd.ACT_SILU])
