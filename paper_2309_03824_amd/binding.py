@@ -418,32 +418,32 @@ class ProfileLog:
         return out
 
 
-def _same(like, shape, *tensors):
-    """Pointers of tensors of `like`'s type and device and of `shape` (None stays None)."""
-    for t in tensors:
-        if t is not None and (t.dtype != like.dtype or t.shape != shape or t.device != like.device):
-            raise ValueError(f"{like.dtype} tensor of shape {tuple(shape)} on {like.device} expected, not {t.dtype} {tuple(t.shape)} on {t.device}")
-    return [_ptr(t) for t in tensors]
+def _device(t) -> int:
+    """The tensors' device, which has to be the current one: a call takes that one's stream."""
+    dev = t.get_device()
+    if dev < 0:
+        raise ValueError("device tensor expected")
+    if dev != torch._C._cuda_getDevice():
+        raise ValueError(f"tensors on cuda:{dev}, but the current device is cuda:{torch._C._cuda_getDevice()}")
+    return dev
 
 
-def _f32s(like, *pairs):
-    """Pointers of fp32 tensors on `like`'s device: (tensor or None, shape) each."""
-    for t, shape in pairs:
-        if t is not None and (t.dtype != torch.float32 or t.shape != shape or t.device != like.device):
-            raise ValueError(f"torch.float32 tensor of shape {tuple(shape)} on {like.device} expected, not {t.dtype} {tuple(t.shape)} on {t.device}")
-    return [_ptr(t) for t, _ in pairs]
+def _at(t, dtype, shape, dev):
+    """Pointer of a contiguous tensor of that type, shape and device (None stays None)."""
+    if t is None:
+        return None
+    if t.dtype is not dtype or t.shape != shape or t.get_device() != dev or not t.is_contiguous():
+        raise ValueError(f"contiguous {dtype} tensor of shape {tuple(shape)} on cuda:{dev} expected, not {t.dtype} {tuple(t.shape)} "
+                         f"with strides {t.stride()} on {t.device}")
+    return t.data_ptr()
 
 
-def _here(t):
-    """The current device, whose stream a call takes, has to be the tensors'."""
-    if t.is_cuda and t.device.index != torch._C._cuda_getDevice():
-        raise ValueError(f"tensors on {t.device}, but the current device is cuda:{torch._C._cuda_getDevice()}")
-
-
-def _rng(like, rng):
-    if rng is not None and (rng.dtype not in (torch.int64, torch.uint64) or rng.numel() != 2 or rng.device != like.device):
-        raise ValueError("rng is two 64-bit integers (seed, call) on the tensors' device")
-    return _ptr(rng)
+def _rng(rng, dev):
+    if rng is None:
+        return None
+    if rng.dtype not in (torch.int64, torch.uint64) or rng.numel() != 2 or rng.get_device() != dev or not rng.is_contiguous():
+        raise ValueError("rng is two 64-bit integers (seed, number of the call) on the tensors' device")
+    return rng.data_ptr()
 
 
 # ------------------------------------------------------------------------------- linear pair
@@ -589,52 +589,32 @@ def linear_gated_workspace_bytes(T, n_in, n_out, r, dtype, freeze_mask=0) -> int
 
 def linear_gated_fwd(X, V_cat, U, bias, A, H_save, act, ws=None, stream=None):
     """A [T, out] = act(Zg) * Zu of a gated pair; U [2, out, r] (the gate's first), V_cat [2r, in], bias [2, out] or None, H_save [T, 2r] or None."""
-    T, n_in = X.shape
-    _, n_out, r = U.shape
-    _here(X)
-    x, = _same(X, (T, n_in), X)
-    v, = _same(X, (2 * r, n_in), V_cat)
-    u, = _same(X, (2, n_out, r), U)
-    a, = _same(X, (T, n_out), A)
-    h, = _same(X, (T, 2 * r), H_save)
-    b, = _f32s(X, (bias, (2, n_out)))
+    (T, n_in), (_, n_out, r), td, dev = X.shape, U.shape, X.dtype, _device(X)
     wp, wb = _ws(ws)
-    _check(_lib.lrd_linear_gated_fwd(x, v, u, b, a, h, act, T, n_in, n_out, r, _dt(X), wp, wb, _stream(stream)), "lrd_linear_gated_fwd")
+    _check(_lib.lrd_linear_gated_fwd(_at(X, td, (T, n_in), dev), _at(V_cat, td, (2 * r, n_in), dev), _at(U, td, (2, n_out, r), dev),
+                                     _at(bias, torch.float32, (2, n_out), dev), _at(A, td, (T, n_out), dev), _at(H_save, td, (T, 2 * r), dev), act, T,
+                                     n_in, n_out, r, _dt(X), wp, wb, _stream(stream)), "lrd_linear_gated_fwd")
 
 
 def linear_gated_bwd(dA, X, H, V_cat, U, bias, dX, dV_cat, dU, dbias, freeze_mask, act, ws=None, stream=None):
     """All gradients of a gated pair from dA [T, out]; H as saved by the forward, or None (computed again from X)."""
-    T, n_out = dA.shape
-    _, _, r = U.shape
-    n_in = V_cat.shape[1]
-    _here(dA)
-    d, = _same(dA, (T, n_out), dA)
-    x, dx = _same(dA, (T, n_in), X, dX)
-    h, = _same(dA, (T, 2 * r), H)
-    v, = _same(dA, (2 * r, n_in), V_cat)
-    u, = _same(dA, (2, n_out, r), U)
-    b, dv, du, db = _f32s(dA, (bias, (2, n_out)), (dV_cat, (2 * r, n_in)), (dU, (2, n_out, r)), (dbias, (2, n_out)))
+    (T, n_out), r, n_in, td, dev, f32 = dA.shape, U.shape[2], V_cat.shape[1], dA.dtype, _device(dA), torch.float32
     wp, wb = _ws(ws)
-    _check(_lib.lrd_linear_gated_bwd(d, x, h, v, u, b, dx, dv, du, db, freeze_mask, act, T, n_in, n_out, r, _dt(dA), wp, wb, _stream(stream)),
+    _check(_lib.lrd_linear_gated_bwd(_at(dA, td, (T, n_out), dev), _at(X, td, (T, n_in), dev), _at(H, td, (T, 2 * r), dev),
+                                     _at(V_cat, td, (2 * r, n_in), dev), _at(U, td, (2, n_out, r), dev), _at(bias, f32, (2, n_out), dev),
+                                     _at(dX, td, (T, n_in), dev), _at(dV_cat, f32, (2 * r, n_in), dev), _at(dU, f32, (2, n_out, r), dev),
+                                     _at(dbias, f32, (2, n_out), dev), freeze_mask, act, T, n_in, n_out, r, _dt(dA), wp, wb, _stream(stream)),
            "lrd_linear_gated_bwd")
 
 
 def linear_gated_bwd_data(dA, H, V_cat, U, bias, dX, dZ, dH_save, act, ws=None, stream=None):
     """Data gradient only; dZ [2, T, out] and dH_save [T, 2r] receive what linear_wgrad_batched takes (dZ in the place of dY)."""
-    T, n_out = dA.shape
-    _, _, r = U.shape
-    n_in = V_cat.shape[1]
-    _here(dA)
-    d, = _same(dA, (T, n_out), dA)
-    h, dh = _same(dA, (T, 2 * r), H, dH_save)
-    v, = _same(dA, (2 * r, n_in), V_cat)
-    u, = _same(dA, (2, n_out, r), U)
-    dx, = _same(dA, (T, n_in), dX)
-    dz, = _same(dA, (2, T, n_out), dZ)
-    b, = _f32s(dA, (bias, (2, n_out)))
+    (T, n_out), r, n_in, td, dev = dA.shape, U.shape[2], V_cat.shape[1], dA.dtype, _device(dA)
     wp, wb = _ws(ws)
-    _check(_lib.lrd_linear_gated_bwd_data(d, h, v, u, b, dx, dz, dh, act, T, n_in, n_out, r, _dt(dA), wp, wb, _stream(stream)),
-           "lrd_linear_gated_bwd_data")
+    _check(_lib.lrd_linear_gated_bwd_data(_at(dA, td, (T, n_out), dev), _at(H, td, (T, 2 * r), dev), _at(V_cat, td, (2 * r, n_in), dev),
+                                          _at(U, td, (2, n_out, r), dev), _at(bias, torch.float32, (2, n_out), dev), _at(dX, td, (T, n_in), dev),
+                                          _at(dZ, td, (2, T, n_out), dev), _at(dH_save, td, (T, 2 * r), dev), act, T, n_in, n_out, r, _dt(dA), wp, wb,
+                                          _stream(stream)), "lrd_linear_gated_bwd_data")
 
 
 def linear_fwd_act(X, V, U, bias, Y, Y_act, H_save, act, ws=None, stream=None):
@@ -726,9 +706,8 @@ def gelu_bwd(dA, Z, dZ, stream=None):
 def dropout(X, Y, p, rng, stream=None):
     """Y = X / (1 - p) where the generator keeps an element, else 0; rng: int64 tensor (seed, number of the call).  The gradient is the
     same call on dY."""
-    _here(X)
-    x, y = _same(X, X.shape, X, Y)
-    _check(_lib.lrd_dropout(x, y, X.numel(), p, _rng(X, rng), _dt(X), _stream(stream)), "lrd_dropout")
+    td, shape, dev = X.dtype, X.shape, _device(X)
+    _check(_lib.lrd_dropout(_at(X, td, shape, dev), _at(Y, td, shape, dev), X.numel(), p, _rng(rng, dev), _dt(X), _stream(stream)), "lrd_dropout")
 
 
 def _gate_rows(opt: "BlockNorm", T, d):
@@ -737,11 +716,13 @@ def _gate_rows(opt: "BlockNorm", T, d):
 
 def block_norm_fwd(F, X, w_post, b_post, gate, w_pre, b_pre, rng, Y, N, opt: "BlockNorm", stream=None):
     """Y = residual_scale X + branch_scale drop(gate * norm_post(F)), N = norm_pre(Y); see lrd_block_norm_fwd for what may be None."""
-    T, d = X.shape
-    _here(X)
-    f, x, y, n = _same(X, (T, d), F, X, Y, N)
-    wo, bo, g, wi, bi = _f32s(X, (w_post, (d,)), (b_post, (d,)), (gate, _gate_rows(opt, T, d)), (w_pre, (d,)), (b_pre, (d,)))
-    _check(_lib.lrd_block_norm_fwd(f, x, wo, bo, g, wi, bi, _rng(X, rng), y, n, ctypes.byref(opt), T, d, _dt(X), _stream(stream)), "lrd_block_norm_fwd")
+    shape, td, dev, f32 = X.shape, X.dtype, _device(X), torch.float32
+    T, d = shape
+    row = (d,)
+    _check(_lib.lrd_block_norm_fwd(_at(F, td, shape, dev), _at(X, td, shape, dev), _at(w_post, f32, row, dev), _at(b_post, f32, row, dev),
+                                   gate if gate is None else _at(gate, f32, _gate_rows(opt, T, d), dev), _at(w_pre, f32, row, dev),
+                                   _at(b_pre, f32, row, dev), _rng(rng, dev), _at(Y, td, shape, dev), _at(N, td, shape, dev), ctypes.byref(opt), T, d,
+                                   _dt(X), _stream(stream)), "lrd_block_norm_fwd")
 
 
 def block_norm_workspace_bytes(T, d) -> int:
@@ -752,12 +733,12 @@ def block_norm_bwd(dY, dN, F, Y, w_post, b_post, gate, w_pre, rng, dX, dF, dw_po
                    stream=None):
     """Gradients of block_norm_fwd from dY and dN (either may be None); see lrd_block_norm_bwd for what may be None."""
     like = dY if dY is not None else dN
-    T, d = like.shape
-    _here(like)
-    dy, dn, f, y, dx, df = _same(like, (T, d), dY, dN, F, Y, dX, dF)
-    gs = _gate_rows(opt, T, d)
-    wo, bo, g, wi = _f32s(like, (w_post, (d,)), (b_post, (d,)), (gate, gs), (w_pre, (d,)))
-    dwo, dbo, dg, dwi, dbi = _f32s(like, (dw_post, (d,)), (db_post, (d,)), (dgate, gs), (dw_pre, (d,)), (db_pre, (d,)))
+    shape, td, dev, f32 = like.shape, like.dtype, _device(like), torch.float32
+    T, d = shape
+    row, gates = (d,), _gate_rows(opt, T, d)
     wp, wb = _ws(ws)
-    _check(_lib.lrd_block_norm_bwd(dy, dn, f, y, wo, bo, g, wi, _rng(like, rng), dx, df, dwo, dbo, dg, dwi, dbi, ctypes.byref(opt), T, d, _dt(like), wp,
-                                   wb, _stream(stream)), "lrd_block_norm_bwd")
+    _check(_lib.lrd_block_norm_bwd(_at(dY, td, shape, dev), _at(dN, td, shape, dev), _at(F, td, shape, dev), _at(Y, td, shape, dev),
+                                   _at(w_post, f32, row, dev), _at(b_post, f32, row, dev), _at(gate, f32, gates, dev), _at(w_pre, f32, row, dev),
+                                   _rng(rng, dev), _at(dX, td, shape, dev), _at(dF, td, shape, dev), _at(dw_post, f32, row, dev),
+                                   _at(db_post, f32, row, dev), _at(dgate, f32, gates, dev), _at(dw_pre, f32, row, dev), _at(db_pre, f32, row, dev),
+                                   ctypes.byref(opt), T, d, _dt(like), wp, wb, _stream(stream)), "lrd_block_norm_bwd")

@@ -8,12 +8,12 @@ hipError_t block_norm_bwd_f32(const BlockNormBwd& g, hipStream_t st) { return di
 
 namespace {
 
-// out[c] = sum over k of src[k][c], a fixed order: four lanes of rows, then their sums in order.
+// out[c] = sum over k of src[k][c], a fixed order: sixteen lanes of rows, then their sums in order.  (Four lanes took 11 us for 512 rows of 1024.)
 struct SumRows { const float* src; float* out; int64_t ld, rows, group_stride, out_stride; };
 struct SumRowsArgs { SumRows job[BN_SUMS + 1]; int64_t first_block[BN_SUMS + 2]; int64_t col_blocks; int d, jobs; };
-__global__ __launch_bounds__(256) void sum_rows_kernel(SumRowsArgs a)
+__global__ __launch_bounds__(1024) void sum_rows_kernel(SumRowsArgs a)
 {
-    __shared__ float part[4][64];
+    __shared__ float part[16][64];
     int j = 0;
     while (j + 1 < a.jobs && (int64_t)blockIdx.x >= a.first_block[j + 1]) ++j;
     const SumRows& s = a.job[j];
@@ -22,12 +22,16 @@ __global__ __launch_bounds__(256) void sum_rows_kernel(SumRowsArgs a)
     float v = 0.f;
     if (c < a.d) {
         const float* at = s.src + group * s.group_stride + c;
-#pragma unroll 4
-        for (int64_t k = l; k < s.rows; k += 4) v += at[k * s.ld];
+#pragma unroll 8
+        for (int64_t k = l; k < s.rows; k += 16) v += at[k * s.ld];
     }
     part[l][threadIdx.x & 63] = v;
     __syncthreads();
-    if (l == 0 && c < a.d) s.out[group * s.out_stride + c] = part[0][threadIdx.x] + part[1][threadIdx.x] + part[2][threadIdx.x] + part[3][threadIdx.x];
+    if (l == 0 && c < a.d) {
+#pragma unroll
+        for (int k = 1; k < 16; ++k) v += part[k][threadIdx.x];
+        s.out[group * s.out_stride + c] = v;
+    }
 }
 
 }  // namespace
@@ -46,7 +50,7 @@ hipError_t block_norm_sums(const BlockNormBwd& g, float* const (&outs)[BN_SUMS],
         if (g.sums[s]) add({g.partial + (int64_t)s * g.d, outs[s], (int64_t)BN_SUMS * g.d, g.workgroups, 0, 0}, 1);
     if (g.dgate && g.parts > 1) add({g.gate_partial, g.dgate, g.d, g.parts, g.parts * g.d, g.d}, g.units / g.parts);
     if (!a.jobs) return hipSuccess;
-    hipLaunchKernelGGL(sum_rows_kernel, dim3((unsigned)blocks), dim3(256), 0, st, a);
+    hipLaunchKernelGGL(sum_rows_kernel, dim3((unsigned)blocks), dim3(1024), 0, st, a);
     return hipGetLastError();
 }
 

@@ -5,7 +5,8 @@
 
 namespace lrd {
 
-enum { BN_W_PRE, BN_B_PRE, BN_W_POST, BN_B_POST, BN_SUMS };     // partial rows of a workgroup
+enum { BN_W_PRE, BN_B_PRE, BN_W_POST, BN_B_POST, BN_SUMS, BN_GATE = BN_SUMS };     // partial rows of a workgroup, and the gate's of a unit
+#define BN_BIT(SUM) (1 << lrd::BN_##SUM)
 
 // Units of rows, none across two rows of the gate: `by_slot`, a group of gate_rows rows each, for one of a workgroup's slots;
 // else `parts` of part_rows rows in each group (the last ones of the last group may be empty), for a workgroup.
@@ -14,28 +15,39 @@ struct BlockNormPlan {
     bool by_slot;
 };
 
-inline int64_t block_norm_slots(int64_t d) { return d <= 1024 ? 8 : 1; }      // rows that a workgroup works on at once
+// Threads of a row: the fewest whose registers hold it, 16 columns each; backward, past a wave's 1024 columns, 8 where rows are no whole groups
+// of 16 bytes, whose code takes more registers (8192 x 4095 505 us with 16 columns, 301 with 8; 8192 x 1001 98 us in a wave, 135 in four).
+inline bool block_norm_ragged(int64_t d, int64_t element) { return d % (16 / element) != 0; }
+inline int block_norm_threads(int64_t d, bool eight)
+{
+    const int64_t most = eight ? 8 : 16;
+    return d <= 1024 ? 64 : d <= 256 * most ? 256 : d <= 512 * most ? 512 : 1024;
+}
+inline int64_t block_norm_slots(int threads) { return threads == 64 ? 8 : 1; }      // rows that a workgroup works on at once
+// Workgroups that run at a time: eight waves a compute unit, or sixteen of those that have 128 registers.  (Twice as many for 8192 x 1024: as many
+// partial rows more, and each workgroup too few rows to load ahead.)
+inline int64_t block_norm_resident(int threads) { return threads == 256 ? 512 : 256; }
 
-inline BlockNormPlan block_norm_plan(int64_t T, int64_t d, int64_t gate_rows)
+inline BlockNormPlan block_norm_plan(int64_t T, int64_t d, int64_t gate_rows, bool ragged)
 {
     auto up = [](int64_t a, int64_t b) { return (a + b - 1) / b; };
-    constexpr int64_t MOST = 512;                   // workgroups: two to a compute unit
-    const int64_t slots = block_norm_slots(d);
+    const int threads = block_norm_threads(d, ragged);
+    const int64_t slots = block_norm_slots(threads), most = block_norm_resident(threads);
     BlockNormPlan p;
     p.gate_rows = gate_rows > 0 && gate_rows < T ? gate_rows : T;
     const int64_t groups = up(T, p.gate_rows);
     p.by_slot = groups > 1 && p.gate_rows <= 16;
     if (p.by_slot) {
         p.units = groups; p.parts = 1; p.part_rows = p.gate_rows;
-        p.workgroups = std::min(MOST, up(groups, slots));
+        p.workgroups = std::min(most, up(groups, slots));
         return p;
     }
     // parts of a group so that there is a unit for each workgroup, and no smaller than a round of its slots
-    const int64_t wanted = up(std::min(MOST, up(T, slots)), groups);
+    const int64_t wanted = up(std::min(most, up(T, slots)), groups);
     p.part_rows = std::max(slots, up(p.gate_rows, wanted));
     p.parts = up(p.gate_rows, p.part_rows);
     p.units = groups * p.parts;
-    p.workgroups = std::min(MOST, p.units);
+    p.workgroups = std::min(most, p.units);
     return p;
 }
 

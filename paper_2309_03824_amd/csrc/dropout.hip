@@ -19,7 +19,7 @@ __global__ __launch_bounds__(256) void dropout_kernel(const T* X, T* Y, int64_t 
     for (int64_t g = (int64_t)blockIdx.x * 256 + threadIdx.x; g < groups; g += stride) {
         T8 v = *reinterpret_cast<const T8*>(X + g * 8);
         if constexpr (DROP) {
-            const uint4 w = key.eight((uint64_t)g);
+            const Words4 w = key.eight((uint64_t)g);
 #pragma unroll
             for (int e = 0; e < 8; ++e) v[e] = drop_bits(w, e) >= rng.below ? (T)((float)v[e] * rng.scale) : (T)0.f;
         }
@@ -28,7 +28,7 @@ __global__ __launch_bounds__(256) void dropout_kernel(const T* X, T* Y, int64_t 
     if (blockIdx.x == 0 && threadIdx.x < n - groups * 8) {
         const int64_t i = groups * 8 + threadIdx.x;
         if constexpr (DROP) {
-            const uint4 w = key.eight((uint64_t)groups);
+            const Words4 w = key.eight((uint64_t)groups);
             Y[i] = drop_bits(w, threadIdx.x) >= rng.below ? (T)((float)X[i] * rng.scale) : (T)0.f;
         } else Y[i] = X[i];
     }

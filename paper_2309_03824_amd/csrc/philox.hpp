@@ -5,8 +5,10 @@
 
 namespace lrd {
 
+struct Words4 { uint32_t w0, w1, w2, w3; };
+
 // Four words for a counter of 128 bits and a key of 64: any element's bits are computed where they are needed.
-__device__ __forceinline__ uint4 philox4x32(uint32_t c0, uint32_t c1, uint32_t c2, uint32_t c3, uint32_t k0, uint32_t k1)
+__device__ __forceinline__ Words4 philox4x32(uint32_t c0, uint32_t c1, uint32_t c2, uint32_t c3, uint32_t k0, uint32_t k1)
 {
 #pragma unroll
     for (int round = 0; round < 10; ++round) {
@@ -18,7 +20,7 @@ __device__ __forceinline__ uint4 philox4x32(uint32_t c0, uint32_t c1, uint32_t c
         k0 += 0x9E3779B9u;
         k1 += 0xBB67AE85u;
     }
-    return make_uint4(c0, c1, c2, c3);
+    return {c0, c1, c2, c3};
 }
 
 // Which elements a dropout keeps.  Element i of the dense array has 16 bits: half (i & 1) of word (i >> 1 & 3) for the counter
@@ -39,12 +41,12 @@ struct DropKey {
         k0 = (uint32_t)seed; k1 = (uint32_t)(seed >> 32);
         c2 = (uint32_t)call; c3 = (uint32_t)(call >> 32);
     }
-    __device__ __forceinline__ uint4 eight(uint64_t group) const { return philox4x32((uint32_t)group, (uint32_t)(group >> 32), c2, c3, k0, k1); }
+    __device__ __forceinline__ Words4 eight(uint64_t group) const { return philox4x32((uint32_t)group, (uint32_t)(group >> 32), c2, c3, k0, k1); }
 };
 // The bits of element e = 0 .. 7 of a group (e known at compile time or not).
-__device__ __forceinline__ uint32_t drop_bits(const uint4& w, int e)
+__device__ __forceinline__ uint32_t drop_bits(Words4 w, int e)
 {
-    const uint32_t v = (e & 4) ? ((e & 2) ? w.w : w.z) : ((e & 2) ? w.y : w.x);
+    const uint32_t lo = (e & 2) ? w.w1 : w.w0, hi = (e & 2) ? w.w3 : w.w2, v = (e & 4) ? hi : lo;
     return (e & 1) ? v >> 16 : v & 0xffffu;
 }
 

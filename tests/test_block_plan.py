@@ -14,7 +14,7 @@ int main()
 {
     long long T, d, g;
     while (scanf("%lld %lld %lld", &T, &d, &g) == 3) {
-        const lrd::BlockNormPlan p = lrd::block_norm_plan(T, d, g);
+        const lrd::BlockNormPlan p = lrd::block_norm_plan(T, d, g, d % 8 != 0);
         printf("%lld %lld %lld %lld %lld %d %lld %lld\n", (long long)p.gate_rows, (long long)p.units, (long long)p.parts, (long long)p.part_rows,
                (long long)p.workgroups, (int)p.by_slot, (long long)lrd::block_norm_most_workgroups(T), (long long)lrd::block_norm_most_units(T));
     }
@@ -37,7 +37,7 @@ def plan(tmp_path_factory):
 
 def test_every_row_is_dealt_once(plan):
     rng = random.Random(5)
-    cases = [(T, d, g) for T in list(range(1, 40)) + [511, 512, 513, 4100, 8192, 100001] for d in (64, 1024, 1025, 16384) for g in (0, 1, 2, 15, 16, 17, 18, 512, T - 1, T, T + 1)]
+    cases = [(T, d, g) for T in list(range(1, 40)) + [511, 512, 513, 4100, 8192, 100001] for d in (64, 513, 1024, 1025, 3000, 16384) for g in (0, 1, 2, 15, 16, 17, 18, 512, T - 1, T, T + 1)]
     cases += [(int(2 ** (rng.random() * 17)) + 1, rng.choice((8, 4096)), int(2 ** (rng.random() * 17))) for _ in range(300)]
     for (T, d, g), (rows, units, parts, part_rows, workgroups, by_slot, most_w, most_u) in zip(cases, plan(cases)):
         what = (T, d, g)
@@ -61,4 +61,4 @@ def test_every_row_is_dealt_once(plan):
 def test_the_largest_counts_of_tokens(plan):
     for (T, d, g), p in zip([(2 ** 31 - 1, 1024, 0), (2 ** 31 - 1, 8192, 1), (2 ** 31 - 1, 64, 4096), (2 ** 31 - 1, 64, 17)],
                             plan([(2 ** 31 - 1, 1024, 0), (2 ** 31 - 1, 8192, 1), (2 ** 31 - 1, 64, 4096), (2 ** 31 - 1, 64, 17)])):
-        assert p[4] == 512 and (p[2] == 1 or p[1] <= p[7]) and p[2] * p[3] >= p[0], (T, d, g, p)
+        assert p[4] in (256, 512) and (p[2] == 1 or p[1] <= p[7]) and p[2] * p[3] >= p[0], (T, d, g, p)
