@@ -708,6 +708,40 @@ __global__ __launch_bounds__(256) void crop_pair_kernel(const float* __restrict_
 }
 }  // namespace
 
+namespace {
+// out[g][c] = sum over t of Z[g][t][c] for two matrices, rows in sixteen lanes, then their sums in order.
+template <class T>
+__global__ __launch_bounds__(1024) void pair_sums_kernel(const T* __restrict__ Z, int64_t rows, int64_t n, int64_t ld, float* __restrict__ out)
+{
+    __shared__ float part[16][64];
+    const int l = threadIdx.x >> 6;
+    const int64_t c = (int64_t)blockIdx.x * 64 + (threadIdx.x & 63);
+    const T* from = Z + blockIdx.y * rows * ld + c;
+    float s = 0.f;
+    if (c < n) {
+#pragma unroll 8
+        for (int64_t t = l; t < rows; t += 16) s += to_f32(from[t * ld]);
+    }
+    part[l][threadIdx.x & 63] = s;
+    __syncthreads();
+    if (l == 0 && c < n) {
+#pragma unroll
+        for (int k = 1; k < 16; ++k) s += part[k][threadIdx.x];
+        out[blockIdx.y * n + c] = s;
+    }
+}
+}  // namespace
+
+bool pair_sums_supported(int64_t T) { return T <= 1024; }
+
+hipError_t pair_sums(const void* Z, int64_t T, int64_t n, int64_t ld, bool bf16, float* out, hipStream_t st)
+{
+    const dim3 grid((unsigned)ceil_div(n, 64), 2);
+    if (bf16) hipLaunchKernelGGL(pair_sums_kernel<bf16_t>, grid, dim3(1024), 0, st, (const bf16_t*)Z, T, n, ld, out);
+    else hipLaunchKernelGGL(pair_sums_kernel<float>, grid, dim3(1024), 0, st, (const float*)Z, T, n, ld, out);
+    return hipGetLastError();
+}
+
 hipError_t crop_pair(const float* src, int64_t rows_s, int64_t cols_s, float* dst, int64_t rows, int64_t cols, hipStream_t st)
 {
     if (rows * cols >= (int64_t(1) << 32)) return hipErrorInvalidValue;

@@ -1024,7 +1024,8 @@ lrd_status lrd_linear_gated_bwd(const void* dA, const void* X, const void* H, co
     p.factors(cv, in, out, r, z.out, z.r);
     float* const gU = train_u && (z.pad_r || z.pad_out) ? (float*)cv.take((size_t)2 * z.out * z.r * 4) : dU;
     float* const gV = train_v && z.pad_r ? (float*)cv.take((size_t)2 * z.r * in * 4) : dV_cat;
-    float* const gb = dbias && z.pad_out ? (float*)cv.take((size_t)2 * z.out * 4) : dbias;
+    const bool one_sum = pair_sums_supported(T);
+    float* const gb = dbias && z.pad_out && !one_sum ? (float*)cv.take((size_t)2 * z.out * 4) : dbias;
     void* Hnew = nullptr;
     if (!H) p.H = Hnew = cv.take((size_t)T * 2 * z.r * esize(dt));
     else if (z.pad_r) p.intermediate(cv, T, r, z.r);
@@ -1042,7 +1043,8 @@ lrd_status lrd_linear_gated_bwd(const void* dA, const void* X, const void* H, co
     GatedOp op = gated_op(p.H, p.U, bias, T, out, z.r, act, dt);
     op.dA = dA; op.dZ = dZ; op.ldz = op.u_rows = z.out;
     LRD_TRY(run_gated(op, st));
-    const lrd_status rc = group_bwd(dZ, X, p.H, p.V, p.U, dX, gV, gU, gb, freeze_mask, T, in, z.out, z.r, 2, dt, rest_at, ws_bytes - cv.used, hip_stream, true);
+    if (dbias && one_sum) LRD_TRY(pair_sums(dZ, T, out, z.out, dt == LRD_BF16, dbias, st));
+    const lrd_status rc = group_bwd(dZ, X, p.H, p.V, p.U, dX, gV, gU, one_sum ? nullptr : gb, freeze_mask, T, in, z.out, z.r, 2, dt, rest_at, ws_bytes - cv.used, hip_stream, true);
     if (rc != LRD_OK) return rc;
     if (gU != dU) LRD_TRY(crop_pair(gU, z.out, z.r, dU, out, r, st));
     if (gb != dbias) LRD_TRY(crop_pair(gb, z.out, 1, dbias, out, 1, st));
