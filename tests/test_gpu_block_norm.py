@@ -94,6 +94,18 @@ def test_every_combination_of_parts(post, pre, gate, bias, p, layer):
         c.check_backward(c.check_forward())
 
 
+@pytest.mark.parametrize("p", [1e-7, 0.999, 1.0])
+def test_nothing_or_everything_dropped(p):
+    c = Case(21, 136, "bf16", p=p, gate_rows=4)
+    c.check_backward(c.check_forward())
+
+
+def test_a_gate_for_more_tokens_than_there_are():
+    for rows in (50, 51, 1000):
+        c = Case(50, 200, "bf16", gate_rows=rows, layer=True)
+        c.check_backward(c.check_forward())
+
+
 @pytest.mark.parametrize("d", [768, 4096, 16384])
 def test_each_gradient_by_itself(d):
     """Whatever else a call asks for, each gradient has the same bits, and what it does not ask for is not written."""
@@ -157,7 +169,7 @@ def test_infinities_and_nan_stay_in_their_row_and_are_dropped_with_their_element
 
 
 def test_results_in_the_place_of_operands():
-    for d in (264, 515, 5000):
+    for d in (264, 515, 5000, 12304, 16001):
         c = Case(40, d, "bf16", p=0.1)
         Y, N = c.forward()
         x, f = c.X.clone(), c.F.clone()
@@ -265,3 +277,32 @@ def test_block_norm_replays():
         step()
         torch.cuda.synchronize()
         assert all(torch.equal(t, w) for t, w in zip(outs, want)), rep
+
+
+def test_rows_past_32_bits():
+    """More than 2^31 elements: the last rows are those of a call on them alone."""
+    d = 1024
+    T = (1 << 31) // d + 300
+    g = torch.Generator(device="cuda").manual_seed(3)
+    F = torch.randn(T, d, device="cuda", dtype=torch.bfloat16, generator=g)
+    X = torch.randn(T, d, device="cuda", dtype=torch.bfloat16, generator=g)
+    gate = torch.randn(-(-T // 1000), d, device="cuda", generator=g)
+    w = torch.rand(d, device="cuda", generator=g) + 0.5
+    rng = torch.tensor([SEED, CALL], dtype=torch.int64, device="cuda")
+    opt = lrd.BlockNorm(dropout_p=0.2, gate_rows=1000)
+    Y, N = torch.empty_like(X), torch.empty_like(X)
+    lrd.block_norm_fwd(F, X, w, None, gate, w, None, rng, Y, N, opt)
+    at = (T - 1) // 1000 * 1000                      # the last group
+    n = T - at
+    factors = ref.drop_factors(n * d, 0.2, SEED, CALL, first=at * d).reshape(n, d)
+    o = dict(layer=False, eps=float(torch.tensor(1e-5)), alpha=1.0, beta=1.0, gate_rows=0)
+    y, nn = ref.block_norm_fwd(host(F[at:]), host(X[at:]), host(w), None, host(gate[-1:]), host(w), None, factors, o)
+    ref.assert_close(Y[at:], y, torch.bfloat16, "Y")
+    ref.assert_close(N[at:], nn, torch.bfloat16, "N")
+    dX, dF, dgate = torch.empty_like(X), N, torch.empty_like(gate)
+    ws = workspace(lrd.block_norm_workspace_bytes(T, d))
+    lrd.block_norm_bwd(X, F, F, Y, w, None, gate, w, rng, dX, dF, None, None, dgate, None, None, opt, ws)
+    want = ref.block_norm_bwd(host(X[at:]), host(F[at:]), host(F[at:]), host(Y[at:]), host(w), None, host(gate[-1:]), host(w), factors, o)
+    ref.assert_close(dX[at:], want["dX"], torch.bfloat16, "dX")
+    ref.assert_close(dF[at:], want["dF"], torch.bfloat16, "dF")
+    ref.assert_close(dgate[-1:], want["dgate"], torch.float32, "dgate")

@@ -192,3 +192,55 @@ def test_gated_replays_and_runs_on_another_stream():
         step()
     side.synchronize()
     assert all(torch.equal(t, w) for t, w in zip(outs, want))
+
+
+@pytest.mark.parametrize("n_out", [8192, 8190])
+def test_results_past_32_bits(n_out):
+    """More than 2^31 results: the last rows against 64 bits, forward and backward."""
+    T, n_in, r, act = (1 << 31) // 8190 + 200, 16, 8, lrd.ACT_SILU
+    g = torch.Generator(device="cuda").manual_seed(1)
+    bf = dict(dtype=torch.bfloat16, device="cuda")
+    X, V, Uc = (torch.randn(*s, generator=g, **bf) for s in ((T, n_in), (2 * r, n_in), (2, n_out, r)))
+    A, H = torch.empty(T, n_out, **bf), torch.empty(T, 2 * r, **bf)
+    ws = workspace(lrd.linear_gated_workspace_bytes(T, n_in, n_out, r, lrd.BF16))
+    lrd.linear_gated_fwd(X, V, Uc, None, A, H, act, ws)
+    k = 150
+    ref.assert_close(A[-k:], ref.gated(host(H[-k:]), host(Uc), None, act, torch.bfloat16), torch.bfloat16, "A")
+    dZ, dH = torch.empty(2, T, n_out, **bf), torch.empty(T, 2 * r, **bf)
+    lrd.linear_gated_bwd_data(A, H, V, Uc, None, None, dZ, dH, act, ws)
+    for i, want in enumerate(ref.gated(host(H[-k:]), host(Uc), None, act, torch.bfloat16, host(A[-k:]))):
+        ref.assert_close(dZ[i, -k:], want, torch.bfloat16, "dZ")
+    c, e = ref.product(host(dZ[1, -k:]), host(Uc)[1].t())
+    ref.assert_close(dH[-k:, r:].contiguous(), (c, ref.SAFE * e), torch.bfloat16, "dH")
+
+
+def test_two_calls_at_once():
+    """Two streams, each with buffers and a workspace of its own."""
+    jobs = []
+    for i, (T, n_in, n_out, r) in enumerate([(1100, 256, 1024, 64), (900, 512, 1000, 61)]):
+        X, V, Uc, b, dA = inputs(T, n_in, n_out, r, "bf16", True, seed=i)
+        bf = dict(dtype=torch.bfloat16, device="cuda")
+        out = dict(A=torch.empty(T, n_out, **bf), H=torch.empty(T, 2 * r, **bf), dX=torch.empty(T, n_in, **bf), dV=torch.empty(2 * r, n_in, device="cuda"),
+                   dU=torch.empty(2, n_out, r, device="cuda"), db=torch.empty(2, n_out, device="cuda"))
+        jobs.append((X, V, Uc, b, dA, out, workspace(lrd.linear_gated_workspace_bytes(T, n_in, n_out, r, lrd.BF16)), torch.cuda.Stream()))
+
+    def step(job):
+        X, V, Uc, b, dA, o, ws, _ = job
+        lrd.linear_gated_fwd(X, V, Uc, b, o["A"], o["H"], lrd.ACT_GELU, ws)
+        lrd.linear_gated_bwd(dA, X, o["H"], V, Uc, b, o["dX"], o["dV"], o["dU"], o["db"], 0, lrd.ACT_GELU, ws)
+    want = []
+    for job in jobs:
+        step(job)
+        torch.cuda.synchronize()
+        want.append({k: v.clone() for k, v in job[5].items()})
+    for _ in range(3):
+        for job in jobs:
+            for v in job[5].values():
+                v.zero_()
+        torch.cuda.synchronize()
+        for job in jobs:
+            with torch.cuda.stream(job[7]):
+                step(job)
+        torch.cuda.synchronize()
+        for job, w in zip(jobs, want):
+            assert all(torch.equal(v, w[k]) for k, v in job[5].items())
