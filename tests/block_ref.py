@@ -87,7 +87,7 @@ def gated(H, Uc, bias, act, dt, dA=None):
         zs.append((z, e))
     (zg, eg), (zu, eu) = zs
     a, da = act_terms(zg, act)
-    ea, eda = act_errors(zg, act, dt)
+    ea, eda = act_errors(zg, act, dt if dA is None else torch.float32)       # (backward in fp32's accuracy whatever the type)
     ea, eda = ea + 1.13 * eg, eda + 0.8 * eg                  # |act'| <= 1.13, |act''| <= 0.8
     if dA is None:
         return a * zu, SAFE * (zu.abs() * ea + a.abs() * eu + ea * eu + 2 * U * (a * zu).abs())
