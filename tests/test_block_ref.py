@@ -186,3 +186,10 @@ def test_workspaces_never_fall():
         for dt in (lrd.BF16, lrd.F32):
             sizes = [lrd.linear_gated_workspace_bytes(T, n_in, n_out, r, dt) for T in list(range(1, 1400)) + list(range(1400, 18000, 37))]
             assert sizes == sorted(sizes)
+
+
+def test_a_gated_pair_at_the_greatest_width_is_not_padded_past_it():
+    """A group has fewer than 2^24 outputs a layer: a pair whose padded width would reach that is computed as it is, without padded copies."""
+    out, r = 2**24 - 1, 8
+    assert 0 < lrd.linear_gated_workspace_bytes(1, 8, out, r, lrd.BF16) < 2 * out * r * 2       # (the bytes of one padded copy of U)
+    assert lrd.linear_gated_workspace_bytes(1, 8, out + 1, r, lrd.BF16) == 0
