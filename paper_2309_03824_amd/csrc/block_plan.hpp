@@ -15,23 +15,18 @@ struct BlockNormPlan {
     bool by_slot;
 };
 
-// Threads of a row: the fewest whose registers hold it, 16 columns each; backward, past a wave's 1024 columns, 8 where rows are no whole groups
-// of 16 bytes, whose code takes more registers (8192 x 4095 505 us with 16 columns, 301 with 8; 8192 x 1001 98 us in a wave, 135 in four).
-inline bool block_norm_ragged(int64_t d, int64_t element) { return d % (16 / element) != 0; }
-inline int block_norm_threads(int64_t d, bool eight)
-{
-    const int64_t most = eight ? 8 : 16;
-    return d <= 1024 ? 64 : d <= 256 * most ? 256 : d <= 512 * most ? 512 : 1024;
-}
+// Threads of a row: the fewest whose registers hold it, 16 columns each.  (8 for rows that are no whole groups of 16 bytes: 8192 x 4095 194 us against
+// 169, 2048 x 8003 175 against 109.)
+inline int block_norm_threads(int64_t d) { return d <= 1024 ? 64 : d <= 4096 ? 256 : d <= 8192 ? 512 : 1024; }
 inline int64_t block_norm_slots(int threads) { return threads == 64 ? 8 : 1; }      // rows that a workgroup works on at once
 // Workgroups that run at a time: eight waves a compute unit, or sixteen of those that have 128 registers.  (Twice as many for 8192 x 1024: as many
 // partial rows more, and each workgroup too few rows to load ahead.)
 inline int64_t block_norm_resident(int threads) { return threads == 256 ? 512 : 256; }
 
-inline BlockNormPlan block_norm_plan(int64_t T, int64_t d, int64_t gate_rows, bool ragged)
+inline BlockNormPlan block_norm_plan(int64_t T, int64_t d, int64_t gate_rows)
 {
     auto up = [](int64_t a, int64_t b) { return (a + b - 1) / b; };
-    const int threads = block_norm_threads(d, ragged);
+    const int threads = block_norm_threads(d);
     const int64_t slots = block_norm_slots(threads), most = block_norm_resident(threads);
     BlockNormPlan p;
     p.gate_rows = gate_rows > 0 && gate_rows < T ? gate_rows : T;

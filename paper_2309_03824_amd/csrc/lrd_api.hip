@@ -1542,7 +1542,7 @@ lrd_status lrd_block_norm_bwd(const void* dY, const void* dN, const void* F, con
         !aligned16(w_pre) || !aligned16(rng) || !aligned16(dX) || !aligned16(dF) || !aligned16(dw_post) || !aligned16(db_post) ||
         !aligned16(dgate) || !aligned16(dw_pre) || !aligned16(db_pre) || !aligned16(ws))
         return LRD_ERR_ALIGNMENT;
-    const BlockNormPlan plan = block_norm_plan(T, d, gate ? opt->gate_rows : 0, block_norm_ragged(d, esize(dt)));
+    const BlockNormPlan plan = block_norm_plan(T, d, gate ? opt->gate_rows : 0);
     Carver cv(ws, ws_bytes);
     const bool rows = dw_pre || db_pre || dw_post || db_post;
     if (rows) g.partial = (float*)cv.take((size_t)plan.workgroups * BN_SUMS * d * 4);

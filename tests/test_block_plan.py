@@ -14,7 +14,7 @@ int main()
 {
     long long T, d, g;
     while (scanf("%lld %lld %lld", &T, &d, &g) == 3) {
-        const lrd::BlockNormPlan p = lrd::block_norm_plan(T, d, g, d % 8 != 0);
+        const lrd::BlockNormPlan p = lrd::block_norm_plan(T, d, g);
         printf("%lld %lld %lld %lld %lld %d %lld %lld\n", (long long)p.gate_rows, (long long)p.units, (long long)p.parts, (long long)p.part_rows,
                (long long)p.workgroups, (int)p.by_slot, (long long)lrd::block_norm_most_workgroups(T), (long long)lrd::block_norm_most_units(T));
     }

@@ -75,6 +75,14 @@ def test_widths(d, dt, layer):
 
 
 @pytest.mark.parametrize("dt", ["bf16", "f32"])
+@pytest.mark.parametrize("d", [2, 4, 5, 7, 9, 10, 15, 17, 31, 255, 257, 505, 519, 1017, 1023, 1025, 1031, 2047, 2049, 2061, 2503, 4097, 8191, 8193, 16379, 16383])
+def test_groups_that_end_with_their_row(d, dt):
+    for T, gate_rows in ((1, 0), (11, 2), (300, 150)):
+        c = Case(T, d, dt, layer=d % 2 == 0, gate_rows=gate_rows, p=0.25)
+        c.check_backward(c.check_forward())
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
 @pytest.mark.parametrize("T,gate_rows", [(1, 0), (1, 1), (2, 1), (9, 2), (33, 3), (100, 16), (100, 17), (700, 99), (700, 699), (1300, 1), (5000, 0), (5000, 2500), (9000, 4)])
 @pytest.mark.parametrize("d", [96, 1032])
 def test_tokens_and_gates(T, gate_rows, d, dt):
