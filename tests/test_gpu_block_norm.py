@@ -192,6 +192,32 @@ def test_results_in_the_place_of_operands():
         assert torch.equal(dy, whole["dX"]) and torch.equal(y, whole["dF"])
 
 
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+@pytest.mark.parametrize("d", [6, 264, 515, 2503, 4096, 9001, 12304])
+def test_gradients_in_the_place_of_any_two_operands(d, dt):
+    c = Case(40, d, dt, p=0.1, layer=True)
+    Y, _ = c.forward()
+    for with_n in (True, False):
+        if not with_n:
+            c.dN = None
+        like = lambda t, there=True: torch.empty_like(t) if there else None
+        ws = workspace(lrd.block_norm_workspace_bytes(40, d))
+
+        def run(dY, dN, F, Y, dX, dF):
+            sums = [like(c.w_post), like(c.b_post), like(c.gate), like(c.w_pre, with_n), like(c.b_pre, with_n)]
+            lrd.block_norm_bwd(dY, dN, F, Y if with_n else None, c.w_post, c.b_post, c.gate, c.w_pre if with_n else None, c.rng, dX, dF, *sums, c.opt, ws)
+            return [dX, dF] + [t for t in sums if t is not None]
+
+        want = run(c.dY, c.dN, c.F, Y, torch.empty_like(Y), torch.empty_like(Y))
+        at = ("dY", "dN", "F", "Y") if with_n else ("dY", "F")
+        for a in at:
+            for b in at:
+                if a != b:
+                    o = dict(dY=c.dY.clone(), dN=None if c.dN is None else c.dN.clone(), F=c.F.clone(), Y=Y.clone())
+                    for x, y in zip(run(*o.values(), o[a], o[b]), want):
+                        assert torch.equal(x, y), (a, b, with_n)
+
+
 def test_rows_past_the_last_token_and_columns_past_a_row_are_left_alone():
     for d in (100, 1536):
         c = Case(13, d, "bf16", gate_rows=5)
