@@ -2,8 +2,6 @@
 // from dA.  Zg and Zu never leave the registers: over a rank they cost less to compute again than to store and load (2 r
 // multiplications against 4 bytes written and read an element).
 #include <algorithm>
-#include <cstdio>
-#include <string>
 
 #include "gated.hpp"
 #include "lds_load.hpp"
