@@ -597,6 +597,10 @@ inline bool group_dims_ok(int64_t T, int64_t in, int64_t out, int64_t r, int32_t
 {
     return groups >= 1 && groups <= 64 && linear_dims_ok(T, in, out, r) && (int64_t)groups * r < (int64_t(1) << 24);
 }
+// dH of a gated pair (the callers that pass one_row) in one launch for both layers, however few the tokens, while the reduction is short: two
+// sliced products and their two sums cost more than the longer reduction.  The data gradient of -> 2048 at rank 256, 64 tokens 19.4 -> 13.6 us, 1248
+// tokens 34.5 -> 24.7; -> 4096 24.0 -> 20.9 and 46.1 -> 39.1; -> 8192 it would go 27.8 -> 35.5 and 67.8 -> 64.7.
+inline bool pair_whole(int64_t out) { return out <= 4096; }
 inline const char* at(const void* p, int64_t elems, lrd_dtype dt) { return (const char*)p + elems * (int64_t)esize(dt); }
 
 size_t group_partial_region(int64_t T, int64_t in, int64_t out, int64_t r, int32_t G, lrd_dtype dt, bool backward,
@@ -675,7 +679,7 @@ lrd_status group_bwd(const void* dY, const void* X, const void* H, const void* V
     if (!cv.ok) return LRD_ERR_WORKSPACE;
 
     if (need_dH) {
-        if (choose_splits_act(T, r, out, dt == LRD_BF16) > 1) {
+        if (!(one_row && pair_whole(out)) && choose_splits_act(T, r, out, dt == LRD_BF16) > 1) {
             // few tokens: each group's product is sliced along K and summed into its columns of dH
             for (int32_t g = 0; g < groups; ++g) {
                 MatOp d1 = nn(at(dY, (int64_t)g * T * out, dt), out, at(U, (int64_t)g * out * r, dt), r, (void*)at(dH, g * r, dt), gr,
@@ -781,7 +785,7 @@ lrd_status group_bwd_data(const void* dY, const void* V_cat, const void* U, void
     const size_t region_bytes = act_partial_bytes(T, r, out, dt);
     void* region = region_bytes ? cv.take(region_bytes) : nullptr;
     if (!cv.ok) return LRD_ERR_WORKSPACE;
-    if (choose_splits_act(T, r, out, dt == LRD_BF16) > 1) {
+    if (!(one_row && pair_whole(out)) && choose_splits_act(T, r, out, dt == LRD_BF16) > 1) {
         for (int32_t g = 0; g < groups; ++g) {
             MatOp d1 = nn(at(dY, (int64_t)g * T * out, dt), out, at(U, (int64_t)g * out * r, dt), r, (void*)at(dH_save, g * r, dt),
                           gr, T, r, out, dt);
