@@ -901,8 +901,9 @@ struct GatedSizes {
 };
 GatedSizes gated_sizes(int64_t in, int64_t out, int64_t r, lrd_dtype dt)
 {
-    // (padded sizes that a group still takes)
-    const bool pads = dt == LRD_BF16 && in % 8 == 0 && pad8(out) < (int64_t(1) << 24) && 2 * pad8(r) < (int64_t(1) << 24);
+    // (padded sizes that a group still takes, and gradients that crop_pair does)
+    const bool pads = dt == LRD_BF16 && in % 8 == 0 && pad8(out) < (int64_t(1) << 24) && 2 * pad8(r) < (int64_t(1) << 24) &&
+                      out * r < (int64_t(1) << 32);
     GatedSizes z{pads ? pad8(r) : r, pads ? pad8(out) : out, false, false};
     z.pad_r = z.r != r;
     z.pad_out = z.out != out;

@@ -193,3 +193,10 @@ def test_a_gated_pair_at_the_greatest_width_is_not_padded_past_it():
     out, r = 2**24 - 1, 8
     assert 0 < lrd.linear_gated_workspace_bytes(1, 8, out, r, lrd.BF16) < 2 * out * r * 2       # (the bytes of one padded copy of U)
     assert lrd.linear_gated_workspace_bytes(1, 8, out + 1, r, lrd.BF16) == 0
+
+
+def test_a_gated_pair_whose_gradients_pass_32_bits_is_not_padded():
+    """Cropping counts a layer's dU in 32 bits: past that a pair is computed at its own sizes."""
+    T, n_in, out, r = 1, 1024, 2**22 + 1, 1024
+    padded = 2 * (out + 7) * r * (2 + 4)                # copies of U and of dU
+    assert 0 < lrd.linear_gated_workspace_bytes(T, n_in, out, r, lrd.BF16) < padded
