@@ -25,4 +25,16 @@ hipError_t pair_sums(const void* Z, int64_t T, int64_t n, int64_t ld, bool bf16,
 // dst [2][rows x cols] = the first rows and columns of src [2][rows_s x cols_s] (fp32).
 hipError_t crop_pair(const float* src, int64_t rows_s, int64_t cols_s, float* dst, int64_t rows, int64_t cols, hipStream_t st);
 
+// out [2][M x N] (fp32, dense): for each of two layers g the sum over T rows of A[t][m] * B[t][n]; A of layer g begins a_bs elements behind the first's, B b_bs.
+struct FewRows {
+    const void* A;
+    int64_t lda, a_bs;
+    const void* B;
+    int64_t ldb, b_bs;
+    float* out;
+    int64_t M, N;
+};
+bool few_rows_supported(int64_t T, int64_t in, int64_t out, int64_t r, bool bf16, bool padded);       // padded: the products need copies at padded sizes
+hipError_t few_rows(const FewRows* jobs, int n, int64_t T, bool bf16, hipStream_t st);       // one or two, in one launch
+
 }  // namespace lrd

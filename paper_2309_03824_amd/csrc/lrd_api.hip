@@ -1028,8 +1028,9 @@ lrd_status lrd_linear_gated_bwd(const void* dA, const void* X, const void* H, co
     Carver cv(ws, ws_bytes);
     GatedPadded p(U, V_cat, H);
     p.factors(cv, in, out, r, z.out, z.r);
-    float* const gU = train_u && (z.pad_r || z.pad_out) ? (float*)cv.take((size_t)2 * z.out * z.r * 4) : dU;
-    float* const gV = train_v && z.pad_r ? (float*)cv.take((size_t)2 * z.r * in * 4) : dV_cat;
+    const bool few = few_rows_supported(T, in, out, r, dt == LRD_BF16, z.pad_r || z.pad_out);
+    float* const gU = !few && train_u && (z.pad_r || z.pad_out) ? (float*)cv.take((size_t)2 * z.out * z.r * 4) : dU;
+    float* const gV = !few && train_v && z.pad_r ? (float*)cv.take((size_t)2 * z.r * in * 4) : dV_cat;
     const bool one_sum = pair_sums_supported(T);
     float* const gb = dbias && z.pad_out && !one_sum ? (float*)cv.take((size_t)2 * z.out * 4) : dbias;
     void* Hnew = nullptr;
@@ -1050,6 +1051,20 @@ lrd_status lrd_linear_gated_bwd(const void* dA, const void* X, const void* H, co
     op.dA = dA; op.dZ = dZ; op.ldz = op.u_rows = z.out;
     LRD_TRY(run_gated(op, st));
     if (dbias && one_sum) LRD_TRY(pair_sums(dZ, T, out, z.out, dt == LRD_BF16, dbias, st));
+    if (few) {
+        Carver rc(rest_at, rest);
+        void* const dH = need_dH ? rc.take((size_t)T * 2 * z.r * esize(dt)) : nullptr;
+        if (dH) {
+            const lrd_status e = group_bwd_data(dZ, p.V, p.U, dX, dH, T, in, z.out, z.r, 2, dt, rest_at + rc.used, rest - rc.used, hip_stream, true);
+            if (e != LRD_OK) return e;
+        }
+        FewRows jobs[2];
+        int n = 0;
+        if (train_u) jobs[n++] = {dZ, z.out, T * z.out, p.H, 2 * z.r, z.r, dU, out, r};
+        if (train_v) jobs[n++] = {dH, 2 * z.r, z.r, X, in, 0, dV_cat, r, in};
+        if (n) LRD_TRY(few_rows(jobs, n, T, dt == LRD_BF16, st));
+        return LRD_OK;
+    }
     const lrd_status rc = group_bwd(dZ, X, p.H, p.V, p.U, dX, gV, gU, one_sum ? nullptr : gb, freeze_mask, T, in, z.out, z.r, 2, dt, rest_at, ws_bytes - cv.used, hip_stream, true);
     if (rc != LRD_OK) return rc;
     if (gU != dU) LRD_TRY(crop_pair(gU, z.out, z.r, dU, out, r, st));

@@ -115,6 +115,40 @@ def test_frozen_factors_and_null_arguments(dt, r):
     assert torch.equal(frozen["dX"], whole["dX"]) and torch.equal(frozen["dU"], whole["dU"])
 
 
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+@pytest.mark.parametrize("n_in,n_out,r", [(64, 96, 24), (64, 96, 29), (200, 131, 70), (65, 67, 31), (8, 4104, 8), (7, 5, 3)])
+@pytest.mark.parametrize("T", [1, 2, 15, 16, 17, 32, 33, 64, 65])
+def test_weight_gradients_of_few_tokens(T, n_in, n_out, r, dt):
+    act, td = lrd.ACT_SILU, TYPES[dt]
+    X, V, Uc, b, dA = inputs(T, n_in, n_out, r, dt, True)
+    ws = workspace(lrd.linear_gated_workspace_bytes(T, n_in, n_out, r, CODE[dt]))
+    new = lambda *s: torch.empty(*s, dtype=td, device="cuda")
+    H, dX, dZ, dH = new(T, 2 * r), new(T, n_in), new(2, T, n_out), new(T, 2 * r)
+    lrd.linear_gated_fwd(X, V, Uc, b, new(T, n_out), H, act, ws)
+    lrd.linear_gated_bwd_data(dA, H, V, Uc, b, dX, dZ, dH, act, ws)
+    hX, hH, hZ, hdH = host(X), host(H), host(dZ), host(dH)
+
+    def grads(mask, want_x=True):
+        u, v = (torch.full((n + 64,), 9.0, device="cuda") for n in (2 * n_out * r, 2 * r * n_in))
+        gX, gb = torch.full_like(X, 9.0), torch.full((2, n_out), 9.0, device="cuda")
+        gU, gV = u[:2 * n_out * r].view(2, n_out, r), v[:2 * r * n_in].view(2 * r, n_in)
+        lrd.linear_gated_bwd(dA, X, H, V, Uc, b, gX if want_x else None, gV, gU, gb, mask, act, ws)
+        assert (u[2 * n_out * r:] == 9).all() and (v[2 * r * n_in:] == 9).all()
+        return dict(dX=gX, dU=gU, dV=gV, db=gb)
+    whole = grads(0)
+    for k in range(2):
+        c, e = ref.product(hZ[k].t(), hH[:, k * r:(k + 1) * r].t())
+        ref.assert_close(whole["dU"][k], (c, ref.SAFE * e), torch.float32, "dU")
+        ref.assert_close(whole["db"][k], (hZ[k].sum(0), ref.SAFE * (T + 2) * ref.U * hZ[k].abs().sum(0)), torch.float32, "dbias")
+    c, e = ref.product(hdH.t(), hX.t())
+    ref.assert_close(whole["dV"], (c, ref.SAFE * e), torch.float32, "dV")
+    c, e = ref.product(hdH, host(V).t())
+    ref.assert_close(whole["dX"], (c, ref.SAFE * e), td, "dX")
+    for mask, x, same, left in ((1, True, ("dX", "dU"), ("dV",)), (2, True, ("dX", "dV"), ("dU",)), (2, False, ("dV",), ("dX", "dU")), (1, False, ("dU",), ("dX", "dV"))):
+        got = grads(mask, x)
+        assert all(torch.equal(got[k], whole[k]) for k in same + ("db",)) and all((got[k] == 9).all() for k in left), (mask, x)
+
+
 def test_batched_weight_gradients_of_a_gated_pair():
     """dZ and dH of the data gradient go into lrd_linear_wgrad_batched as a stack's backward puts them there."""
     T, n_in, n_out, r, L, act = 264, 128, 192, 32, 3, lrd.ACT_GELU
