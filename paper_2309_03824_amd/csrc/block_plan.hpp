@@ -15,6 +15,15 @@ struct BlockNormPlan {
     bool by_slot;
 };
 
+// Workgroups of a forward pass, a row or a few each, in two dimensions: a launch counts the threads of one in 32 bits (2^26 rows of a wave each, 2^24
+// of 256 threads).  The last row of the grid may be longer than what is left.
+struct RowsGrid { uint32_t x, y; };
+inline RowsGrid rows_grid(int64_t workgroups, int threads)
+{
+    const int64_t most = ((int64_t(1) << 32) - 1) / threads, y = (workgroups + most - 1) / most;
+    return {(uint32_t)((workgroups + y - 1) / y), (uint32_t)y};
+}
+
 // Threads of a row: the fewest whose registers hold it, 16 columns each.  (8 for rows that are no whole groups of 16 bytes: 8192 x 4095 194 us against
 // 169, 2048 x 8003 175 against 109.)
 inline int block_norm_threads(int64_t d) { return d <= 1024 ? 64 : d <= 4096 ? 256 : d <= 8192 ? 512 : 1024; }
