@@ -4,6 +4,7 @@
 #include <algorithm>
 
 #include "gated.hpp"
+#include "gated_plan.hpp"
 #include "lds_load.hpp"
 #include "lrd.h"
 #include "lrd_internal.hpp"
@@ -377,10 +378,8 @@ hipError_t launch_deep(const GatedOp& op, hipStream_t st)
     return hipGetLastError();
 }
 
-enum Route { DIRECT_16, DIRECT_32, WIDE, DEEP, TILES };
-
 template <class T, int ACT, bool BACK>
-hipError_t launch(const GatedOp& op, Route how, hipStream_t st)
+hipError_t launch(const GatedOp& op, GatedRoute how, hipStream_t st)
 {
     GatedArgs<T> g;
     g.H = (const T*)op.H; g.U = (const T*)op.U; g.bias = op.bias; g.dA = (const T*)op.dA; g.A = (T*)op.A; g.dZ = (T*)op.dZ;
@@ -412,6 +411,7 @@ constexpr int COLS = 64;             // columns of a chunk
 constexpr int ROWS = 32;             // rows of a wave
 constexpr int SUB = COLS * 64 * 2;   // LDS bytes of 64 k of a chunk of one factor
 constexpr int WAVES = 4;
+static_assert(ROWS * WAVES == GATED_WIDE_ROWS && COLS == GATED_WIDE_COLS && 64 * WAVES == GATED_WIDE_THREADS, "as planned");
 constexpr int AUX_NT = 2;            // non-temporal: results are too many for the caches
 
 struct GatedWideArgs {
@@ -663,27 +663,10 @@ hipError_t wide_by_depth(const GatedOp& op, hipStream_t st)
     }
 }
 
-// Which kernel, by the number of workgroups that it gives work (us a call by itself, T x out x r with SiLU, forward):
-//   16 x 16 blocks up to 512 of them (64 x 1024 x 256 6.2, in 32 x 32 ones 6.8, wide 8.4; 64 x 4096 8.8, 7.1, 8.5; fp32 64 x 1024 6.7, 9.6, in tiles 24.0);
-//   32 x 32 blocks up to 512 of them, or 1024 where the wide kernel does not take the call (512 x 1024 x 256 9.0, wide 9.8; 256 x 4096 12.8, 10.0;
-//   256 x 2730 11.0, deep 13.4, in tiles 11.9; 506 x 2730 x 416 19.8, 17.8, 24.2; fp32 512 x 2048 25.2, in tiles 25.7, 1024 x 2048 45.0, 35.3);
-//   then wide, else deep (8192 x 4096 x 256 43, deep 73, in tiles 80; x 1024 deep 226, in tiles 307), else tiles.
-Route route(const GatedOp& op)
-{
-    auto tiles = [&](int64_t e) { return ceil_div(op.T, e) * ceil_div(op.out, e); };
-    // (32-bit byte offsets within 32 rows of a result and 64 columns of a factor; within 128 rows of H or U)
-    const bool wide = op.bf16 && op.r % 8 == 0 && op.r <= 512 && op.out % 8 == 0 && op.ldz == op.out && op.out <= BUF_MAX_LD &&
-                      ceil_div(op.T, ROWS * WAVES) * ceil_div(op.out, COLS) < (int64_t(1) << 31);
-    const bool deep = op.bf16 && op.r % 8 == 0 && op.r <= (int64_t(1) << 21) && tiles(128) < (int64_t(1) << 31);
-    if (tiles(16) <= 512) return DIRECT_16;
-    if (tiles(32) <= (wide ? 512 : 1024)) return DIRECT_32;
-    return wide ? WIDE : deep ? DEEP : TILES;
-}
-
 template <int ACT, bool BACK>
 hipError_t by_type(const GatedOp& op, hipStream_t st)
 {
-    const Route how = route(op);
+    const GatedRoute how = gated_route(op.T, op.out, op.r, op.ldz != op.out, op.bf16, BUF_MAX_LD);
     if (how == WIDE) return op.bias ? wide_by_depth<ACT, BACK, true>(op, st) : wide_by_depth<ACT, BACK, false>(op, st);
     if (how == DEEP) return launch_deep<ACT, BACK>(op, st);
     return op.bf16 ? launch<bf16_t, ACT, BACK>(op, how, st) : launch<float, ACT, BACK>(op, how, st);
@@ -827,7 +810,7 @@ int64_t few_rows_blocks(int64_t M, int64_t N) { return ceil_div(M, 64) * ceil_di
 // 41.2, 64 47.8 and 46.9; fp32 64 tokens -> 4096 at rank 384 66.4 and 70.6, at rank 193 62.1 and 61.3.
 bool few_rows_supported(int64_t T, int64_t in, int64_t out, int64_t r, bool bf16, bool padded)
 {
-    return T <= (!bf16 ? 64 : padded ? 32 : 16) && few_rows_blocks(out, r) + few_rows_blocks(r, in) < (int64_t(1) << 30);
+    return T <= (!bf16 ? 64 : padded ? 32 : 16) && few_rows_blocks(out, r) + few_rows_blocks(r, in) < (int64_t(1) << 23);      // (threads of both layers: 32 bits)
 }
 
 hipError_t few_rows(const FewRows* jobs, int n, int64_t T, bool bf16, hipStream_t st)
