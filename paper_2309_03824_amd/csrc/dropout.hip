@@ -12,7 +12,8 @@ namespace {
 template <class T, bool DROP>
 __global__ __launch_bounds__(256) void dropout_kernel(const T* X, T* Y, int64_t n, DropRng rng)      // Y may be X
 {
-    typedef T T8 __attribute__((ext_vector_type(8)));
+    typedef T Eight __attribute__((ext_vector_type(8)));
+    typedef Eight T8 __attribute__((aligned(16)));          // (what the call asks of X and Y; eight of fp32 would be taken to begin on 32 bytes)
     const int64_t groups = n / 8, stride = (int64_t)gridDim.x * 256;
     DropKey key;
     if constexpr (DROP) key = DropKey(rng.state);
