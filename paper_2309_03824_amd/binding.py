@@ -438,6 +438,15 @@ def _at(t, dtype, shape, dev):
     return t.data_ptr()
 
 
+def _room(ws, dev):
+    """Pointer and bytes of a workspace, which has to be the tensors' device's, without strides (its bytes are counted by its elements)."""
+    if ws is None:
+        return None, 0
+    if ws.get_device() != dev or not ws.is_contiguous():
+        raise ValueError(f"contiguous workspace on cuda:{dev} expected, not {tuple(ws.shape)} with strides {ws.stride()} on {ws.device}")
+    return ws.data_ptr(), ws.numel() * ws.element_size()
+
+
 def _rng(rng, dev):
     if rng is None:
         return None
@@ -590,7 +599,7 @@ def linear_gated_workspace_bytes(T, n_in, n_out, r, dtype, freeze_mask=0) -> int
 def linear_gated_fwd(X, V_cat, U, bias, A, H_save, act, ws=None, stream=None):
     """A [T, out] = act(Zg) * Zu of a gated pair; U [2, out, r] (the gate's first), V_cat [2r, in], bias [2, out] or None, H_save [T, 2r] or None."""
     (T, n_in), (_, n_out, r), td, dev = X.shape, U.shape, X.dtype, _device(X)
-    wp, wb = _ws(ws)
+    wp, wb = _room(ws, dev)
     _check(_lib.lrd_linear_gated_fwd(_at(X, td, (T, n_in), dev), _at(V_cat, td, (2 * r, n_in), dev), _at(U, td, (2, n_out, r), dev),
                                      _at(bias, torch.float32, (2, n_out), dev), _at(A, td, (T, n_out), dev), _at(H_save, td, (T, 2 * r), dev), act, T,
                                      n_in, n_out, r, _dt(X), wp, wb, _stream(stream)), "lrd_linear_gated_fwd")
@@ -599,7 +608,7 @@ def linear_gated_fwd(X, V_cat, U, bias, A, H_save, act, ws=None, stream=None):
 def linear_gated_bwd(dA, X, H, V_cat, U, bias, dX, dV_cat, dU, dbias, freeze_mask, act, ws=None, stream=None):
     """All gradients of a gated pair from dA [T, out]; H as saved by the forward, or None (computed again from X)."""
     (T, n_out), r, n_in, td, dev, f32 = dA.shape, U.shape[2], V_cat.shape[1], dA.dtype, _device(dA), torch.float32
-    wp, wb = _ws(ws)
+    wp, wb = _room(ws, dev)
     _check(_lib.lrd_linear_gated_bwd(_at(dA, td, (T, n_out), dev), _at(X, td, (T, n_in), dev), _at(H, td, (T, 2 * r), dev),
                                      _at(V_cat, td, (2 * r, n_in), dev), _at(U, td, (2, n_out, r), dev), _at(bias, f32, (2, n_out), dev),
                                      _at(dX, td, (T, n_in), dev), _at(dV_cat, f32, (2 * r, n_in), dev), _at(dU, f32, (2, n_out, r), dev),
@@ -610,7 +619,7 @@ def linear_gated_bwd(dA, X, H, V_cat, U, bias, dX, dV_cat, dU, dbias, freeze_mas
 def linear_gated_bwd_data(dA, H, V_cat, U, bias, dX, dZ, dH_save, act, ws=None, stream=None):
     """Data gradient only; dZ [2, T, out] and dH_save [T, 2r] receive what linear_wgrad_batched takes (dZ in the place of dY)."""
     (T, n_out), r, n_in, td, dev = dA.shape, U.shape[2], V_cat.shape[1], dA.dtype, _device(dA)
-    wp, wb = _ws(ws)
+    wp, wb = _room(ws, dev)
     _check(_lib.lrd_linear_gated_bwd_data(_at(dA, td, (T, n_out), dev), _at(H, td, (T, 2 * r), dev), _at(V_cat, td, (2 * r, n_in), dev),
                                           _at(U, td, (2, n_out, r), dev), _at(bias, torch.float32, (2, n_out), dev), _at(dX, td, (T, n_in), dev),
                                           _at(dZ, td, (2, T, n_out), dev), _at(dH_save, td, (T, 2 * r), dev), act, T, n_in, n_out, r, _dt(dA), wp, wb,
@@ -736,7 +745,7 @@ def block_norm_bwd(dY, dN, F, Y, w_post, b_post, gate, w_pre, rng, dX, dF, dw_po
     shape, td, dev, f32 = like.shape, like.dtype, _device(like), torch.float32
     T, d = shape
     row, gates = (d,), _gate_rows(opt, T, d)
-    wp, wb = _ws(ws)
+    wp, wb = _room(ws, dev)
     _check(_lib.lrd_block_norm_bwd(_at(dY, td, shape, dev), _at(dN, td, shape, dev), _at(F, td, shape, dev), _at(Y, td, shape, dev),
                                    _at(w_post, f32, row, dev), _at(b_post, f32, row, dev), _at(gate, f32, gates, dev), _at(w_pre, f32, row, dev),
                                    _rng(rng, dev), _at(dX, td, shape, dev), _at(dF, td, shape, dev), _at(dw_post, f32, row, dev),
