@@ -742,6 +742,8 @@ def block_norm_bwd(dY, dN, F, Y, w_post, b_post, gate, w_pre, rng, dX, dF, dw_po
                    stream=None):
     """Gradients of block_norm_fwd from dY and dN (either may be None); see lrd_block_norm_bwd for what may be None."""
     like = dY if dY is not None else dN
+    if like is None:
+        raise ValueError("dY or dN expected")
     shape, td, dev, f32 = like.shape, like.dtype, _device(like), torch.float32
     T, d = shape
     row, gates = (d,), _gate_rows(opt, T, d)

@@ -51,3 +51,8 @@ def test_a_workspace_on_the_host_is_refused():
     with pytest.raises(ValueError):
         lrd._room(torch.empty(4096, dtype=torch.uint8), 0)
     assert lrd._room(None, 0) == (None, 0)
+
+
+def test_a_backward_pass_without_a_gradient_is_refused(on_host):
+    with pytest.raises(ValueError):
+        lrd.block_norm_bwd(None, None, X, X, W, None, None, W, None, X, A, None, None, None, None, None, lrd.BlockNorm())
